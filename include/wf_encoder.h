@@ -486,6 +486,114 @@ int wf_beam_pruner_reset(wf_beam_pruner *p, const int32_t *ref_tokens, int32_t n
 int wf_beam_prune_session(wf_beam_pruner *p, const int32_t *best_tokens, int32_t n, int32_t *beam_for_step, int32_t *events);
 void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
 
+/* ---- Token-by-token decoding: caches, attention over them, beams -----------------------------------------
+ * What runs on the GPU for every new token after wf_prefill.  Operators on caller-provided DEVICE buffers like wf_op_linear and its kind,
+ * all asynchronous on hip_stream, none allocates, waits or copies, so they can be captured into a graph.  What changes from
+ * step to step (lengths, rows, parents) is read from device memory, so that one captured graph serves every step; the host arguments are
+ * upper bounds.  Device values that lie outside their bounds never lead to an access outside the buffers: such rows or slots are
+ * left out, as stated with each operator.  All work of a call is ordered on its stream; two calls may overlap if their outputs and
+ * workspaces are their own.
+ *
+ * A cache holds keys and values of n_heads heads of size 64 in n_rows rows:
+ *   WF_DTYPE_F32, WF_DTYPE_BF16   data_dev [n_rows, 2 * 64 * n_heads]: the keys of all heads, then the values (a layer of wf_cross_kv's or
+ *                 wf_prefill's buffers is such a cache as it stands); exps_dev is NULL;
+ *   WF_DTYPE_F8   data_dev [n_rows, n_heads, 2, 64] e4m3 (OCP, no infinity): of each head 64 key values, then 64 values; exps_dev uint8
+ *                 [2 * n_heads, n_rows]: entry (2 h, r) for the keys, (2 h + 1, r) for the values of head h in row r.  A stored q stands for
+ *                 q * 2^(exponent - 127).
+ * data_dev is aligned to 16 bytes.  A sequence is a range of consecutive rows; where the ranges of two sequences overlap, writing both in
+ * one call leaves either's values there.
+ *
+ * wf_op_cache_write   token t of sequence s, cu_dev[s] <= t < cu_dev[s + 1] (DEVICE int32 [B+1] prefix sums), goes to row
+ *                     row_dev[s] + t - cu_dev[s] (DEVICE int32 [B]).  k_dev, v_dev: [n_tokens, 64 * n_heads] of dtype f32 or bf16, row stride
+ *                     ld elements (>= 64 * n_heads; both pointers and ld * element size multiples of 16 bytes).  F8: each head's key and
+ *                     value vector gets the smallest power of two 2^e >= 2^-127 with max|x| <= 448 * 2^e and is rounded to nearest even;
+ *                     a value that is not finite is stored as NaN and does not count in the maximum.  Others: rounded to nearest even.
+ *                     Tokens at or behind cu_dev[B] and rows outside the cache are left out; other rows stay as they were.
+ * wf_op_cache_read    the same rows back: out_dev [n_tokens, 2 * 64 * n_heads] (keys of all heads, then values) of dtype f32 or bf16, contiguous.
+ *                     Tokens behind the last sequence keep what out_dev holds; those whose row lies outside the cache read as zero.
+ * wf_op_cache_attention   out[r, h, :] = sum_k w_k v_k, w = softmax over the visible keys k of scale * q[r, h, :] . k.  Row r of q, cu_q_dev[s] <= r
+ *                     < cu_q_dev[s + 1], belongs to sequence s and sees its keys 0 .. len_dev[s] - 1, rows row_dev[s] + k of the cache.  With
+ *                     mask_dev (uint32 [n_q_rows, mask_words]) a key k >= mask_from_dev[s] (NULL: 0) is seen only if bit
+ *                     (k - mask_from_dev[s]) of row r's words is set (bit 0 = lowest bit of word 0; keys behind the last bit are not seen):
+ *                     the tokens of a drafted tree, or of beams that share one cache, see their ancestors.  A row that sees no key gives
+ *                     zeros, and what keys hold that a row does not see (infinities, NaN) does not reach it.  Query head h reads key / value
+ *                     head h / (n_heads / cache->n_heads).  q and out: dtype f32 or bf16, the cache's own or, over an F8 cache, either; strides
+ *                     ldq, ldo in elements; q_dev, out_dev and both strides in bytes are multiples of 16 bytes.  max_q and max_len bound the
+ *                     queries and keys of a sequence: len_dev[s] counts as max_len where it is larger, and as what the cache has from
+ *                     row_dev[s] on; rows of a sequence behind its first max_q, and rows behind the last sequence, are left as they were.
+ *                     workspace_dev: at least wf_cache_attention_workspace(..) bytes (0: may be NULL), aligned to 16, of any content.
+ * wf_op_beam_select   one step of a beam search, per stream s of B with n_in[s] beams (DEVICE int32 [B]; NULL: width; clamped to 0 .. width):
+ *                     candidates (b, t) of all beams b and tokens t with total(b, t) = score_in[s, b] + logits[s, b, t] - log sum exp
+ *                     logits[s, b, :], in 64 bits.  The n_out[s] (NULL: width) best come out, best first: tokens of one beam by
+ *                     their logits and then the lowest token, beams among each other by the totals and then the lowest beam.  logits_dev
+ *                     [B, width, n_vocab] f32 or bf16 with row stride ld elements (a multiple of nothing); logits and scores that are not finite
+ *                     take no part.  done_in (uint8 [B, width], NULL: none): a beam that is done has one candidate, token eos at its
+ *                     own score.  token_out, parent_out int32, score_out f32, done_out uint8 (NULL if done_in is), [B, width]: slots without a
+ *                     candidate hold -1, -1, -infinity, 0; done_out = the parent was done or the token is eos.  keep_slots != 0: the
+ *                     same candidates, ordered so that of each parent's children the best stays in the parent's slot (where that is one
+ *                     of the n_out[s]) and the others fill the free slots from the lowest, best first: wf_op_beam_reorder then moves only slots
+ *                     whose beam died.  score_out may be score_in, done_out may be done_in.  1 <= width <= 32.  workspace_dev: at least
+ *                     wf_beam_select_workspace(..) bytes, aligned to 16, of any content.
+ * wf_op_beam_reorder  slot (s, j) of every layer takes over slot (s, parent[s, j]): a slot is n_pos positions of pos_bytes bytes, slot (s, j) of layer
+ *                     l starts at byte (l * B * width + s * width + j) * n_pos * pos_bytes of src_dev and dst_dev, and the first
+ *                     len_dev[s] positions (DEVICE int32 [B]; NULL: n_pos; clamped to 0 .. n_pos) are moved.  dst_dev == src_dev works in
+ *                     place, for any parents; otherwise the two must not overlap.  A parent outside 0 .. width - 1 leaves dst's slot as it was.
+ */
+#define WF_DTYPE_F8 2
+
+typedef struct {
+  void *data_dev;
+  uint8_t *exps_dev;            /* WF_DTYPE_F8 only */
+  int64_t n_rows;               /* 1 .. 2^31 - 1 */
+  int32_t n_heads;              /* key / value heads, of size 64; 1 .. 1024 */
+  int32_t dtype;                /* WF_DTYPE_* */
+} wf_cache;
+
+typedef struct {
+  const void *q_dev;            /* [n_q_rows, 64 * n_heads], row stride ldq elements */
+  void *out_dev;                /* the same shape and type, row stride ldo */
+  int64_t ldq, ldo;
+  const int32_t *cu_q_dev;      /* [n_seqs + 1] */
+  const int32_t *row_dev;       /* [n_seqs] */
+  const int32_t *len_dev;       /* [n_seqs] */
+  const uint32_t *mask_dev;     /* [n_q_rows, mask_words] or NULL */
+  const int32_t *mask_from_dev; /* [n_seqs] or NULL */
+  void *workspace_dev;
+  int64_t workspace_bytes;
+  int32_t dtype;                /* of q and out: WF_DTYPE_F32, WF_DTYPE_BF16 */
+  int32_t n_heads;              /* query heads, a multiple of the cache's */
+  int32_t n_seqs, n_q_rows, max_q, max_len;
+  int32_t mask_words;
+  float scale;                  /* finite */
+} wf_cache_query;
+
+typedef struct {
+  const void *logits_dev;       /* [B, width, n_vocab], row stride ld elements */
+  int64_t ld;
+  const int32_t *n_in_dev, *n_out_dev;     /* [B] or NULL */
+  const float *score_in_dev;    /* [B, width] */
+  const uint8_t *done_in_dev;   /* [B, width] or NULL */
+  int32_t *token_out_dev, *parent_out_dev;
+  float *score_out_dev;
+  uint8_t *done_out_dev;
+  void *workspace_dev;
+  int64_t workspace_bytes;
+  int32_t dtype;                /* of the logits: WF_DTYPE_F32, WF_DTYPE_BF16 */
+  int32_t B, width, n_vocab, eos, keep_slots;
+} wf_beam_step;
+
+int wf_op_cache_write(const wf_cache *cache, const void *k_dev, const void *v_dev, int32_t dtype, int64_t ld, const int32_t *cu_dev,
+                      const int32_t *row_dev, int32_t B, int32_t n_tokens, void *hip_stream);
+int wf_op_cache_read(const wf_cache *cache, const int32_t *cu_dev, const int32_t *row_dev, int32_t B, void *out_dev, int32_t dtype,
+                     int32_t n_tokens, void *hip_stream);
+/* Bytes of workspace a wf_op_cache_attention call with these arguments needs (host only; pointers are not looked at); negative WF_E_*. */
+int64_t wf_cache_attention_workspace(const wf_cache *cache, const wf_cache_query *query);
+int wf_op_cache_attention(const wf_cache *cache, const wf_cache_query *query, void *hip_stream);
+int64_t wf_beam_select_workspace(const wf_beam_step *step);      /* likewise */
+int wf_op_beam_select(const wf_beam_step *step, void *hip_stream);
+int wf_op_beam_reorder(void *dst_dev, const void *src_dev, const int32_t *parent_dev, const int32_t *len_dev, int32_t B, int32_t width,
+                       int32_t n_layers, int64_t n_pos, int64_t pos_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,7 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libwf_encoder.so")
 
 WF_OK, WF_E_INVALID_ARG, WF_E_CAPACITY, WF_E_OOM, WF_E_HIP = 0, -1, -2, -3, -4
-WF_DTYPE_F32, WF_DTYPE_BF16 = 0, 1
+WF_DTYPE_F32, WF_DTYPE_BF16, WF_DTYPE_F8 = 0, 1, 2
 WF_PRECISION_BF16, WF_PRECISION_F32 = 0, 1
 
 _fp = C.POINTER(C.c_float)
@@ -83,6 +83,26 @@ class WfRoundRecord(C.Structure):
                 ("tokens", C.c_int64), ("n_active", C.c_int32), ("reserved", C.c_int32)]
 
 
+class WfCache(C.Structure):
+    _fields_ = [("data_dev", C.c_void_p), ("exps_dev", C.c_void_p), ("n_rows", C.c_int64), ("n_heads", C.c_int32), ("dtype", C.c_int32)]
+
+
+class WfCacheQuery(C.Structure):
+    _fields_ = [("q_dev", C.c_void_p), ("out_dev", C.c_void_p), ("ldq", C.c_int64), ("ldo", C.c_int64), ("cu_q_dev", C.c_void_p),
+                ("row_dev", C.c_void_p), ("len_dev", C.c_void_p), ("mask_dev", C.c_void_p), ("mask_from_dev", C.c_void_p),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_int64), ("dtype", C.c_int32), ("n_heads", C.c_int32),
+                ("n_seqs", C.c_int32), ("n_q_rows", C.c_int32), ("max_q", C.c_int32), ("max_len", C.c_int32), ("mask_words", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class WfBeamStep(C.Structure):
+    _fields_ = [("logits_dev", C.c_void_p), ("ld", C.c_int64), ("n_in_dev", C.c_void_p), ("n_out_dev", C.c_void_p),
+                ("score_in_dev", C.c_void_p), ("done_in_dev", C.c_void_p), ("token_out_dev", C.c_void_p), ("parent_out_dev", C.c_void_p),
+                ("score_out_dev", C.c_void_p), ("done_out_dev", C.c_void_p), ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_int64),
+                ("dtype", C.c_int32), ("B", C.c_int32), ("width", C.c_int32), ("n_vocab", C.c_int32), ("eos", C.c_int32),
+                ("keep_slots", C.c_int32)]
+
+
 class WfError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"wf error {code}: {msg}")
@@ -101,7 +121,9 @@ EXPORTS = ["wf_encoder_create", "wf_encode_batch", "wf_encoder_destroy", "wf_las
            "wf_rounds_destroy", "wf_run_rounds",
            "wf_beam_pruner_create", "wf_beam_pruner_step", "wf_beam_pruner_reset", "wf_beam_prune_session",
            "wf_beam_pruner_destroy", "wf_op_attention_noalloc",
-           "wf_encoder_set_graphs", "wf_encoder_graph_stats", "wf_gemm_tile_map", "wf_gemm_tile_choice", "wf_gemm_kernel_choice", "wf_gemm_small_choice", "wf_attention_form", "wf_encode_route", "wf_gelu_host", "wf_device_info", "wf_op_ln_linear"]
+           "wf_encoder_set_graphs", "wf_encoder_graph_stats", "wf_gemm_tile_map", "wf_gemm_tile_choice", "wf_gemm_kernel_choice", "wf_gemm_small_choice", "wf_attention_form", "wf_encode_route", "wf_gelu_host", "wf_device_info", "wf_op_ln_linear",
+           "wf_op_cache_write", "wf_op_cache_read", "wf_cache_attention_workspace", "wf_op_cache_attention", "wf_beam_select_workspace",
+           "wf_op_beam_select", "wf_op_beam_reorder"]
 
 
 def lib() -> C.CDLL:
@@ -177,6 +199,17 @@ def lib() -> C.CDLL:
     L.wf_rounds_destroy.restype = None
     L.wf_run_rounds.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
                                 C.c_int32, C.c_int64, C.POINTER(WfRoundRecord), C.c_void_p]
+    L.wf_op_cache_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32,
+                                    C.c_int32, C.c_void_p]
+    L.wf_op_cache_read.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]
+    L.wf_cache_attention_workspace.argtypes = [C.c_void_p, C.c_void_p]
+    L.wf_cache_attention_workspace.restype = C.c_int64
+    L.wf_op_cache_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+    L.wf_beam_select_workspace.argtypes = [C.c_void_p]
+    L.wf_beam_select_workspace.restype = C.c_int64
+    L.wf_op_beam_select.argtypes = [C.c_void_p, C.c_void_p]
+    L.wf_op_beam_reorder.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64,
+                                     C.c_int64, C.c_void_p]
     _lib = L
     return L
 
@@ -685,4 +718,205 @@ def op_ln_linear(x, g, b, w, bias, out, epilogue: int, eps: float = 1e-5, stream
     _check(lib().wf_op_ln_linear(C.c_void_p(x.data_ptr()), C.c_void_p(g.data_ptr()), C.c_void_p(b.data_ptr()), eps,
                                  C.c_void_p(w.data_ptr()), C.c_void_p(bias.data_ptr()), C.c_void_p(out.data_ptr()), M, N, K, epilogue,
                                  C.c_void_p(s)))
+    return out
+
+
+# ---- token-by-token decoding: caches, attention over them, beams -------------------------------
+def _on_device(*tensors, dtype=None, what="tensor"):
+    """The tensors' common device is the current one (a launch goes to the current device's stream) and their type is `dtype`."""
+    import torch
+    here = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda or t.device.index != here:
+            raise ValueError(f"{what} is on {t.device}, need the current CUDA device")
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError(f"{what} is {t.dtype}, need {dtype}")
+
+
+def _index(t, n: int, what: str):
+    """Address of an int32 device array of n values (None: NULL)."""
+    import torch
+    if t is None:
+        return None
+    _on_device(t, dtype=torch.int32, what=what)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {tuple(t.shape)}, need {n} contiguous values")
+    return t.data_ptr()
+
+
+def _rows_2d(t, what: str):
+    """A matrix [rows, columns] whose rows are contiguous; a third dimension (heads, 64) is folded.  Returns (rows, columns, row stride)."""
+    _on_device(t, what=what)
+    if t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] <= 1 or t.stride(1) == t.shape[2]):
+        n, cols = t.shape[0], t.shape[1] * t.shape[2]
+    elif t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
+        n, cols = t.shape
+    else:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, strides {t.stride()}: need rows of contiguous values")
+    return n, cols, max(t.stride(0), cols) if n <= 1 else t.stride(0)
+
+
+def _empty(shape, dtype, device, stream):
+    """Uninitialised memory that belongs to the stream the call goes to (torch's allocator hands memory on in stream order)."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class Cache:
+    """Keys and values of heads of size 64 on the device (wf_cache): `data` [n_rows, 128 n_heads] float32 or bfloat16 (keys of all heads, then
+    values: a layer of what Decoder.cross_kv or prefill returns), or [n_rows, n_heads, 2, 64] float8_e4m3fn with `exps` uint8 [2 n_heads, n_rows]."""
+
+    def __init__(self, data, exps=None):
+        import torch
+        f8 = data.dtype == torch.float8_e4m3fn
+        code = WF_DTYPE_F8 if f8 else _torch_dtype_code(data.dtype)
+        _on_device(data, what="data")
+        if not data.is_contiguous() or data.dim() != (4 if f8 else 2) or (data.shape[2:] != (2, 64) if f8 else data.shape[1] % 128):
+            raise ValueError(f"data: {tuple(data.shape)} with strides {data.stride()}, need [n_rows, 128 n_heads] or, in 8 bits, [n_rows, n_heads, 2, 64]")
+        if f8 != (exps is not None):
+            raise ValueError("exps goes with float8_e4m3fn data and with no other")
+        self.n_rows, self.n_heads = data.shape[0], data.shape[1] if f8 else data.shape[1] // 128
+        if f8:
+            _on_device(exps, dtype=torch.uint8, what="exps")
+            if tuple(exps.shape) != (2 * self.n_heads, self.n_rows) or not exps.is_contiguous():
+                raise ValueError(f"exps: {tuple(exps.shape)}, need [{2 * self.n_heads}, {self.n_rows}]")
+        self.data, self.exps = data, exps
+        self._c = WfCache(data.data_ptr(), exps.data_ptr() if f8 else None, self.n_rows, self.n_heads, code)
+        self._at = C.addressof(self._c)
+
+    @classmethod
+    def empty(cls, n_rows: int, n_heads: int, dtype, device="cuda") -> "Cache":
+        """A cache of zeros."""
+        import torch
+        if dtype == torch.float8_e4m3fn:
+            return cls(torch.zeros((n_rows, n_heads, 2, 64), dtype=torch.uint8, device=device).view(dtype),
+                       torch.zeros((2 * n_heads, n_rows), dtype=torch.uint8, device=device))
+        return cls(torch.zeros((n_rows, 128 * n_heads), dtype=dtype, device=device))
+
+
+def op_cache_write(cache: Cache, k, v, cu, rows, stream=None) -> Cache:
+    """Token t of sequence s (cu[s] <= t < cu[s + 1]) into cache row rows[s] + t - cu[s].  k, v: [n_tokens, 64 n_heads] or [n_tokens, n_heads,
+    64], views into wider rows (a projection's output) with one row stride; cu [B + 1], rows [B]: int32 on the device."""
+    n, cols, ld = _rows_2d(k, "k")
+    if _rows_2d(v, "v") != (n, cols, ld) or v.dtype != k.dtype or cols != 64 * cache.n_heads:
+        raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}: need two [n_tokens, {64 * cache.n_heads}] of one type and row stride")
+    B = rows.numel()
+    _check(lib().wf_op_cache_write(cache._at, k.data_ptr(), v.data_ptr(), _torch_dtype_code(k.dtype), ld, _index(cu, B + 1, "cu"),
+                                   _index(rows, B, "rows"), B, n, _raw_stream(stream)))
+    return cache
+
+
+def op_cache_read(cache: Cache, cu, rows, n_tokens: int, out=None, out_dtype=None, stream=None):
+    """The rows op_cache_write fills, as [n_tokens, 128 n_heads] (keys of all heads, then values)."""
+    import torch
+    if out is None:
+        out = _empty((n_tokens, 128 * cache.n_heads), out_dtype or torch.bfloat16, cache.data.device, stream)
+    _on_device(out, what="out")
+    if tuple(out.shape) != (n_tokens, 128 * cache.n_heads) or not out.is_contiguous():
+        raise ValueError(f"out: {tuple(out.shape)}, need a contiguous [{n_tokens}, {128 * cache.n_heads}]")
+    B = rows.numel()
+    _check(lib().wf_op_cache_read(cache._at, _index(cu, B + 1, "cu"), _index(rows, B, "rows"), B, out.data_ptr(), _torch_dtype_code(out.dtype),
+                                  n_tokens, _raw_stream(stream)))
+    return out
+
+
+def op_cache_attention(cache: Cache, q, cu_q, rows, lens, max_q: int, max_len: int, scale: float = 0.125, mask=None, mask_from=None,
+                       out=None, workspace=None, stream=None):
+    """Softmax attention of the queries [cu_q[s], cu_q[s + 1]) over cache rows rows[s] .. rows[s] + lens[s] - 1.  q: [n_q_rows, 64 n_heads] or
+    [n_q_rows, n_heads, 64]; cu_q [B + 1], rows, lens [B]: int32 on the device; max_q, max_len: upper bounds of a sequence's queries and keys.
+    mask: int32 [n_q_rows, words], bit k - mask_from[s] (mask_from: int32 [B], None: 0) says whether a row sees key k; keys before
+    mask_from[s] are seen by all."""
+    import torch
+    n, cols, ldq = _rows_2d(q, "q")
+    if cols % 64:
+        raise ValueError(f"q: {cols} columns, need 64 for each head")
+    if out is None:       # rows that belong to no sequence are not written
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    n_out, cols_out, ldo = _rows_2d(out, "out")
+    if (n_out, cols_out) != (n, cols) or out.dtype != q.dtype:
+        raise ValueError(f"out: {tuple(out.shape)} {out.dtype}, need {tuple(q.shape)} {q.dtype}")
+    B = rows.numel()
+    words = 0
+    if mask is not None:
+        _on_device(mask, dtype=torch.int32, what="mask")
+        if mask.dim() != 2 or mask.shape[0] != n or not mask.is_contiguous():
+            raise ValueError(f"mask: {tuple(mask.shape)}, need a contiguous [{n}, words]")
+        words = mask.shape[1]
+    a = WfCacheQuery(q.data_ptr(), out.data_ptr(), ldq, ldo, _index(cu_q, B + 1, "cu_q"), _index(rows, B, "rows"), _index(lens, B, "lens"),
+                     mask.data_ptr() if mask is not None else None, _index(mask_from, B, "mask_from"), None, 0, _torch_dtype_code(q.dtype),
+                     cols // 64, B, n, max_q, max_len, words, scale)
+    at = C.addressof(a)
+    workspace = _fill_workspace(a, lib().wf_cache_attention_workspace(cache._at, at), workspace, q.device, stream)
+    _check(lib().wf_op_cache_attention(cache._at, at, _raw_stream(stream)))
+    return out
+
+
+def _fill_workspace(a, need: int, workspace, device, stream):
+    """Sets the call's workspace, its own where the caller gives none; the result has to live until the call is made."""
+    import torch
+    _check(min(need, 0))
+    if workspace is None and need:
+        workspace = _empty(need, torch.uint8, device, stream)
+    if workspace is not None:
+        _on_device(workspace, what="workspace")
+        a.workspace_dev, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size() if workspace.is_contiguous() else 0
+    return workspace
+
+
+def op_beam_select(logits, scores, n_in=None, n_out=None, done=None, eos: int = -1, keep_slots: bool = False, workspace=None, stream=None):
+    """One step of a beam search: logits [B, width, n_vocab] (float32 or bfloat16, rows contiguous), scores float32 [B, width], n_in / n_out int32
+    [B] (None: width), done bool or uint8 [B, width] (None: no beam is done).  Returns (tokens, parents int32, scores float32, done or None),
+    [B, width] each; keep_slots: a parent's best child stays in the parent's slot."""
+    import torch
+    _on_device(logits, what="logits")
+    _on_device(scores, dtype=torch.float32, what="scores")
+    if logits.dim() != 3 or (logits.stride(2) != 1 and logits.shape[2] != 1):
+        raise ValueError(f"logits: {tuple(logits.shape)} with strides {logits.stride()}, need [B, width, n_vocab] with contiguous rows")
+    B, W, V = logits.shape
+    ld = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
+    if B > 1 and W > 1 and logits.stride(0) != W * ld:
+        raise ValueError(f"logits: strides {logits.stride()}, need one row stride over streams and beams")
+    for t in (scores, done):
+        if t is not None and (tuple(t.shape) != (B, W) or not t.is_contiguous()):
+            raise ValueError(f"scores, done: {tuple(t.shape)}, need a contiguous [{B}, {W}]")
+    if done is not None:
+        _on_device(done, what="done")
+        if done.dtype not in (torch.bool, torch.uint8):
+            raise TypeError(f"done is {done.dtype}, need bool or uint8")
+    dev = logits.device
+    token, parent = _empty((B, W), torch.int32, dev, stream), _empty((B, W), torch.int32, dev, stream)
+    score = _empty((B, W), torch.float32, dev, stream)
+    done_out = _empty((B, W), done.dtype, dev, stream) if done is not None else None
+    a = WfBeamStep(logits.data_ptr(), ld, _index(n_in, B, "n_in"), _index(n_out, B, "n_out"), scores.data_ptr(),
+                   done.data_ptr() if done is not None else None, token.data_ptr(), parent.data_ptr(), score.data_ptr(),
+                   done_out.data_ptr() if done is not None else None, None, 0, _torch_dtype_code(logits.dtype), B, W, V, eos, 1 if keep_slots else 0)
+    at = C.addressof(a)
+    workspace = _fill_workspace(a, lib().wf_beam_select_workspace(at), workspace, dev, stream)
+    _check(lib().wf_op_beam_select(at, _raw_stream(stream)))
+    return token, parent, score, done_out
+
+
+def op_beam_reorder(state, parents, lens=None, out=None, stream=None):
+    """Slot (s, j) of every layer takes over slot (s, parents[s, j]).  state: contiguous [n_layers, B * width, n_pos, ..] of any type; parents int32
+    [B, width]; lens int32 [B]: positions in use (None: all).  In place unless `out` is given."""
+    if out is None:
+        out = state
+    _on_device(state, out, what="state")
+    if parents.dim() != 2 or state.dim() < 3 or state.shape[1] != parents.numel():
+        raise ValueError(f"state: {tuple(state.shape)}, parents: {tuple(parents.shape)}: need [n_layers, B * width, n_pos, ..] and [B, width]")
+    if not state.is_contiguous() or not out.is_contiguous() or out.shape != state.shape or out.dtype != state.dtype:
+        raise ValueError("state and out must be contiguous and of one shape and type")
+    B, W = parents.shape
+    pos_bytes = state.element_size()
+    for n in state.shape[3:]:
+        pos_bytes *= n
+    if pos_bytes == 0 or parents.numel() == 0:
+        return out
+    _check(lib().wf_op_beam_reorder(out.data_ptr(), state.data_ptr(), _index(parents, B * W, "parents"), _index(lens, B, "lens"), B, W,
+                                    state.shape[0], state.shape[2], pos_bytes, _raw_stream(stream)))
     return out
