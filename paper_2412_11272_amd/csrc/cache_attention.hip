@@ -1,13 +1,40 @@
 // Attention of a few queries per sequence over a key / value cache (one new token, the beams of a stream, a tree of drafted tokens).  The
 // definition is stated with wf_op_cache_attention in include/wf_encoder.h.
+//
+// Bound by memory: a key / value pair of a head is 256 bytes in bf16 (130 in 8 bits) and serves only the query rows that share the
+// head (queries of the sequence times query heads per key head), so the cache goes from memory straight to registers, once,
+// and nothing of it through the LDS.  A workgroup has one key / value head of one sequence, up to 16 * NQ of its query rows and a range of keys; its
+// waves take tiles of 32 keys in turn, each with a running maximum and sum of its own, and join in the LDS at the end.
+//
+// A tile's products, on the 16 x 16 matrix instructions, run transposed like those of the prefill attention: S^T = K Q^T, O^T = V^T P^T.
+// A lane (n = lane % 16, g = lane / 16) then holds
+//   K as loaded       key 16 s + n of the tile (s = 0, 1), values 16 g .. 16 g + 15: consecutive bytes; which values meet in one instruction is
+//                     free as long as the queries' registers follow (value 16 g + 8 f + i at place i of the f-th instruction)
+//   S^T               query n, keys 16 s + 4 g + i, i = 0 .. 3, so that a query's maximum is four registers, twice, and two exchanges
+//   P^T               the same registers: place 4 s + i of the lane's share of the second product's reduction is key 16 s + 4 g + i
+//   V as loaded       values 4 n .. 4 n + 3 of those same eight keys: consecutive bytes, 16 lanes a whole row of the head
+//   O^T               query n, values 16 g + 4 i + t from the t-th of four instructions (which takes value 4 n + t of each lane's keys)
+// What remains between loading V and multiplying is to pair two keys' values in a register: one byte permutation for two of them.
+//
+// Rounding: logits, statistics and sums are fp32.  Next to bf16 the weights enter as the sum of two bf16 parts (2^-17 of a weight is lost, where
+// one part would lose 2^-9): twice the second product's instructions, of which the kernel has plenty to spare.  The 8-bit caches' powers
+// of two multiply logits and weights, exactly.
 #include "cache_device.h"
 #include "host_runtime.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace wf {
 
 namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 32;      // keys
+constexpr int kMaxSplits = 64;
 
 struct AttendArgs {
   CacheView c;
@@ -17,66 +44,503 @@ struct AttendArgs {
   const int32_t *cu_q, *row, *len;
   const uint32_t *mask;
   const int32_t *mask_from;
-  int32_t n_heads, n_seqs, n_q_rows, max_q, max_len, mask_words;
+  float *part;                       // [sequence][key head][row][split][64], then the maxima and sums [..][split][2]
+  float *part_ml;
+  int32_t n_heads, group, n_seqs, n_q_rows, max_q, max_len, mask_words;
+  int32_t chunks, n_split, split_keys;      // query row chunks of a head, ranges of split_keys keys
   float scale;
 };
 
-template <int CACHE>
-__device__ __forceinline__ float cache_value(const CacheView &c, int64_t r, int h, int kv, int i) {
-  if constexpr (CACHE == WF_DTYPE_F8)
-    return __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)c.data)[((r * c.n_heads + h) * 2 + kv) * 64 + i], 0) * f8_factor(c.exps[(2 * h + kv) * c.n_rows + r]);
-  else if constexpr (CACHE == WF_DTYPE_BF16)
-    return (float)((const __bf16 *)c.data)[(r * 2 + kv) * c.n_heads * 64 + h * 64 + i];
-  else
-    return ((const float *)c.data)[(r * 2 + kv) * c.n_heads * 64 + h * 64 + i];
-}
-
-// One wave per (sequence, query, head): 64 keys at a time, first a lane per key, then a lane per value.
-template <typename T, int CACHE>
-__global__ void __launch_bounds__(64) cache_attention_kernel(AttendArgs p) {
-  __shared__ float sq[64], sw[64];
-  const int lane = threadIdx.x;
-  const int h = blockIdx.x % p.n_heads, i = (blockIdx.x / p.n_heads) % p.max_q, s = blockIdx.x / (p.n_heads * p.max_q);
-  const int64_t r = (int64_t)p.cu_q[s] + i;
-  if (r >= p.cu_q[s + 1] || r < 0 || r >= p.n_q_rows) return;
-  const int hk = h / (p.n_heads / p.c.n_heads);
-  const int64_t row0 = p.row[s];
+// The keys of sequence s: their number and the first row.
+__device__ __forceinline__ int sequence_keys(const AttendArgs &p, int s, int64_t *row0) {
+  *row0 = p.row[s];
   int64_t n = p.len[s];
   n = n < p.max_len ? n : p.max_len;
-  if (row0 < 0) n = 0;
-  n = n < p.c.n_rows - row0 ? n : p.c.n_rows - row0;
-  const int64_t from = !p.mask ? n : p.mask_from ? p.mask_from[s] : 0;
-  sq[lane] = (float)((const T *)p.q)[r * p.ldq + h * 64 + lane];
-  __syncthreads();
-  const float c = p.scale * 1.4426950408889634f;
-  float m = -INFINITY, l = 0.0f, o = 0.0f;
-  for (int64_t k0 = 0; k0 < n; k0 += 64) {
-    const int64_t k = k0 + lane;
-    bool seen = k < n;
-    if (seen && k >= from) {
-      const int64_t at = k - from;
-      seen = at < 32 * (int64_t)p.mask_words && (p.mask[r * p.mask_words + at / 32] >> (at & 31) & 1);
+  if (*row0 < 0) n = 0;
+  n = n < p.c.n_rows - *row0 ? n : p.c.n_rows - *row0;
+  return n > 0 ? (int)n : 0;
+}
+__device__ __forceinline__ int sequence_queries(const AttendArgs &p, int s, int *first) {
+  const int a = p.cu_q[s], b = p.cu_q[s + 1];
+  *first = a;
+  if (a < 0 || b <= a) return 0;
+  int64_t n = (int64_t)b - a;
+  n = n < p.max_q ? n : p.max_q;
+  n = n < (int64_t)p.n_q_rows - a ? n : (int64_t)p.n_q_rows - a;
+  return n > 0 ? (int)n : 0;
+}
+
+template <int CACHE> struct Format;
+template <> struct Format<WF_DTYPE_BF16> { static constexpr int es = 2; };
+template <> struct Format<WF_DTYPE_F32> { static constexpr int es = 4; };
+template <> struct Format<WF_DTYPE_F8> { static constexpr int es = 1; };
+
+// What a lane holds of a tile (see above), and of the masks and exponents that go with it.
+template <int CACHE, int NQ, bool MASK>
+struct Tile {
+  static constexpr int KD = 4 * Format<CACHE>::es, VD = Format<CACHE>::es;      // registers a key sub-tile, a value row
+  uint32_t k[2][KD], v[8][VD];
+  uint32_t ke[CACHE == WF_DTYPE_F8 ? 2 : 1], ve[CACHE == WF_DTYPE_F8 ? 2 : 1];      // four exponents each
+  uint32_t word[MASK ? NQ : 1][2];
+};
+
+template <int N>
+__device__ __forceinline__ void load_dwords(uint32_t (&d)[N], const unsigned char *base, uint32_t at) {
+  if constexpr (N >= 4) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const u32x4 x = *(const u32x4 *)(base + at + 4 * i);
+      d[i] = x[0]; d[i + 1] = x[1]; d[i + 2] = x[2]; d[i + 3] = x[3];
     }
-    float x = -INFINITY;
-    if (seen) {
-      x = 0.0f;
-      for (int d = 0; d < 64; ++d) x += sq[d] * cache_value<CACHE>(p.c, row0 + k, hk, 0, d);
-      x *= c;
-    }
-    const uint64_t some = __ballot(seen);
-    if (!some) continue;
-    const float m_new = fmaxf(m, wave_max(x)), base = m_new == -INFINITY ? 0.0f : m_new;
-    const float w = seen ? exp2f(x - base) : 0.0f, keep = exp2f(m - base);
-    l = l * keep + wave_sum(w);
-    m = m_new;
-    o *= keep;
-    sw[lane] = w;
-    __syncthreads();
-    for (int j = 0; j < 64; ++j)
-      if (some >> j & 1) o += sw[j] * cache_value<CACHE>(p.c, row0 + k0 + j, hk, 1, lane);
-    __syncthreads();
+  } else if constexpr (N == 2) {
+    const u32x2 x = *(const u32x2 *)(base + at);
+    d[0] = x[0]; d[1] = x[1];
+  } else {
+    d[0] = *(const uint32_t *)(base + at);
   }
-  ((T *)p.out)[r * p.ldo + h * 64 + lane] = (T)(l != 0.0f ? o / l : 0.0f);
+}
+
+__device__ __forceinline__ uint32_t pack(bf16x2 x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ uint32_t f8_pair(uint32_t x, bool high) {
+  return pack(high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
+}
+__device__ __forceinline__ float byte_value(uint32_t x, int i) {
+  return i == 0 ? __builtin_amdgcn_cvt_f32_fp8(x, 0) : i == 1 ? __builtin_amdgcn_cvt_f32_fp8(x, 1) : i == 2 ? __builtin_amdgcn_cvt_f32_fp8(x, 2)
+                                                                                               : __builtin_amdgcn_cvt_f32_fp8(x, 3);
+}
+__device__ __forceinline__ bool is_finite(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7f800000u) != 0x7f800000u; }
+
+__device__ __forceinline__ f32x4 mma(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 c) {
+  const u32x4 x = {a[0], a[1], a[2], a[3]}, y = {b[0], b[1], b[2], b[3]};
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+}
+
+// A wave's running state for 16 query rows: lane (n, g) has row n's maximum (in powers of two), its share of the sum, and values 16 g + 4 i + t.
+struct State {
+  float m, l;
+  f32x4 o[4];
+};
+
+template <typename T, int CACHE, int NQ, int NW, bool MASK>
+__global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int es = Format<CACHE>::es;
+  typedef Tile<CACHE, NQ, MASK> Tile;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+  const int H = p.c.n_heads;
+  int id = blockIdx.x;
+  const int h = id % H; id /= H;
+  const int s = id % p.n_seqs; id /= p.n_seqs;
+  const int chunk = id % p.chunks, z = id / p.chunks;
+
+  int q_first;
+  const int rows = sequence_queries(p, s, &q_first) * p.group - chunk * 16 * NQ;      // of this chunk on
+  if (rows <= 0) return;
+  int64_t row0;
+  const int n = sequence_keys(p, s, &row0);
+  const int64_t split_from = (int64_t)z * p.split_keys;
+  if (z > 0 && split_from >= n) return;
+  const int t_end = (int)(((split_from + p.split_keys < n ? split_from + p.split_keys : n) + kTile - 1) / kTile);      // split_keys is a multiple of a tile
+  const int t_first = (int)(split_from / kTile) + wave;
+  const int n_tiles_q = rows >= 16 * NQ ? NQ : (rows + 15) / 16;
+
+  const uint32_t row_bytes = H * 128u * es;
+  const unsigned char *seq = (const unsigned char *)p.c.data + row0 * row_bytes + (CACHE == WF_DTYPE_F8 ? h * 128 : h * 64 * es);
+  const uint32_t v_off = CACHE == WF_DTYPE_F8 ? 64u : H * 64u * es;
+  const uint8_t *k_exps = CACHE == WF_DTYPE_F8 ? p.c.exps + 2 * h * p.c.n_rows + row0 : nullptr;
+  const uint8_t *v_exps = CACHE == WF_DTYPE_F8 ? k_exps + p.c.n_rows : nullptr;
+
+  // The lane's query of each of the 16-row tiles
+  uint32_t qr[NQ][BF ? 8 : 16];
+  const uint32_t *words[MASK ? NQ : 1];
+  (void)words;
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    const int local = t * 16 + n16;
+    const bool have = local < rows;
+    const int row = chunk * 16 * NQ + (have ? local : 0);
+    const int64_t r = q_first + row / p.group;
+    const unsigned char *src = (const unsigned char *)p.q + (r * p.ldq + (h * p.group + row % p.group) * 64 + 16 * g) * sizeof(T);
+    load_dwords(qr[t], src, 0);
+    if (!have)
+#pragma unroll
+      for (int i = 0; i < (BF ? 8 : 16); ++i) qr[t][i] = 0;
+    if constexpr (MASK) words[t] = p.mask + r * p.mask_words;
+  }
+  const int from = MASK && p.mask_from ? p.mask_from[s] : 0;
+
+  const uint32_t k_lane = n16 * row_bytes + g * 16 * es, v_lane = 4 * g * row_bytes + v_off + n16 * 4 * es;
+  auto load = [&](Tile &a, int tile) {
+    const unsigned char *base = seq + (int64_t)tile * kTile * row_bytes;
+    const int left = n - tile * kTile;
+    if (left >= kTile) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) load_dwords(a.k[u], base + 16 * u * row_bytes, k_lane);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) load_dwords(a.v[j], base + (16 * (j >> 2) + (j & 3)) * row_bytes, v_lane);
+      if constexpr (CACHE == WF_DTYPE_F8)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          __builtin_memcpy(&a.ke[u], k_exps + tile * kTile + 16 * u + 4 * g, 4);
+          __builtin_memcpy(&a.ve[u], v_exps + tile * kTile + 16 * u + 4 * g, 4);
+        }
+    } else {                          // keys behind the last are the last again, their values are zero
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int key = 16 * u + n16;
+        load_dwords(a.k[u], base, (key < left ? key : left - 1) * row_bytes + g * 16 * es);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int key = 16 * (j >> 2) + 4 * g + (j & 3);
+        load_dwords(a.v[j], base, (key < left ? key : left - 1) * row_bytes + v_off + n16 * 4 * es);
+        if (key >= left)
+#pragma unroll
+          for (int i = 0; i < Tile::VD; ++i) a.v[j][i] = 0;
+      }
+      if constexpr (CACHE == WF_DTYPE_F8)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          a.ke[u] = a.ve[u] = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = 16 * u + 4 * g + i, at = tile * kTile + (key < left ? key : left - 1);
+            a.ke[u] |= (uint32_t)k_exps[at] << (8 * i);
+            a.ve[u] |= (uint32_t)v_exps[at] << (8 * i);
+          }
+        }
+    }
+    if constexpr (MASK) {             // the two words that hold the tile's 32 bits
+      const int64_t at = (int64_t)tile * kTile - from;
+      const int64_t w = at >> 5;
+      if (at > -kTile) {
+#pragma unroll
+        for (int t = 0; t < NQ; ++t)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) a.word[t][i] = w + i >= 0 && w + i < p.mask_words ? words[t][w + i] : w + i < 0 ? ~0u : 0u;
+      }
+    }
+  };
+  // Bit k: the lane's query of tile t sees key k of the tile
+  auto seen_keys = [&](const Tile &a, int tile, int t) -> uint32_t {
+    const int left = n - tile * kTile;
+    uint32_t w = left >= kTile ? ~0u : (1u << left) - 1;
+    if constexpr (MASK) {
+      const int64_t at = (int64_t)tile * kTile - from;
+      if (at > -kTile) w &= (uint32_t)((((uint64_t)a.word[t][1] << 32) | a.word[t][0]) >> (at & 31));
+    }
+    return w;
+  };
+
+  State st[NQ];
+  const float c = p.scale * 1.4426950408889634f;      // exp(s scale) = exp2(s c)
+  auto reset = [&] {
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      st[t].m = -INFINITY;
+      st[t].l = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st[t].o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  };
+
+  auto compute = [&](const Tile &a, int tile, auto careful) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    // ---- values: pairs of keys next to each other
+    uint32_t vt[4][BF ? 4 : 8];
+    if constexpr (BF) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (CACHE == WF_DTYPE_F8) {
+          const uint32_t x = __builtin_amdgcn_perm(a.v[2 * j + 1][0], a.v[2 * j][0], 0x05010400), y = __builtin_amdgcn_perm(a.v[2 * j + 1][0], a.v[2 * j][0], 0x07030602);
+          vt[0][j] = f8_pair(x, false); vt[1][j] = f8_pair(x, true);
+          vt[2][j] = f8_pair(y, false); vt[3][j] = f8_pair(y, true);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            vt[2 * i][j] = __builtin_amdgcn_perm(a.v[2 * j + 1][i], a.v[2 * j][i], 0x05040100);
+            vt[2 * i + 1][j] = __builtin_amdgcn_perm(a.v[2 * j + 1][i], a.v[2 * j][i], 0x07060302);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          if constexpr (CACHE == WF_DTYPE_F8) vt[t][j] = __builtin_bit_cast(uint32_t, byte_value(a.v[j][0], t));
+          else vt[t][j] = a.v[j][t];
+        }
+    }
+    // ---- keys
+    uint32_t kt[2][BF ? 8 : 16];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (CACHE == WF_DTYPE_F8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (BF) { kt[u][2 * i] = f8_pair(a.k[u][i], false); kt[u][2 * i + 1] = f8_pair(a.k[u][i], true); }
+          else
+#pragma unroll
+            for (int b = 0; b < 4; ++b) kt[u][4 * i + b] = __builtin_bit_cast(uint32_t, byte_value(a.k[u][i], b));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < (BF ? 8 : 16); ++i) kt[u][i] = a.k[u][i];
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      if (t > 0 && t >= n_tiles_q) break;
+      State &w = st[t];
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x4 d{0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (BF) {
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+            const uint32_t ka[4] = {kt[u][4 * f], kt[u][4 * f + 1], kt[u][4 * f + 2], kt[u][4 * f + 3]};
+            const uint32_t qa[4] = {qr[t][4 * f], qr[t][4 * f + 1], qr[t][4 * f + 2], qr[t][4 * f + 3]};
+            d = mma(ka, qa, d);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            d = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kt[u][i]), __builtin_bit_cast(float, qr[t][i]), d, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[4 * u + i] = d[i] * c;
+          if constexpr (CACHE == WF_DTYPE_F8) x[4 * u + i] *= f8_factor((a.ke[u] >> (8 * i)) & 0xff);
+        }
+      }
+      uint32_t seen = ~0u;
+      if (MASK || CAREFUL || n - tile * kTile < kTile) {
+        seen = seen_keys(a, tile, t);
+        const uint32_t mine = seen >> (4 * g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (!(mine >> (16 * (j >> 2) + (j & 3)) & 1)) x[j] = -INFINITY;
+      }
+      float top = x[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
+      const Pair rp = row_pair(top);
+      top = fmaxf(w.m, half_max(fmaxf(rp.a, rp.b)));
+      if (__ballot(top > w.m)) {
+        const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - top);
+        w.l *= keep;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w.o[i] *= keep;
+        w.m = top;
+      }
+      const float base = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] = __builtin_amdgcn_exp2f(x[j] - base);
+        sum += x[j];
+        if constexpr (CACHE == WF_DTYPE_F8) x[j] *= f8_factor((a.ve[j >> 2] >> (8 * (j & 3))) & 0xff);
+      }
+      w.l += sum;
+      uint32_t hi[4], lo[4];
+      if constexpr (BF) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bf16x2 b = {(__bf16)x[2 * j], (__bf16)x[2 * j + 1]};
+          const bf16x2 r = {(__bf16)(x[2 * j] - (float)b[0]), (__bf16)(x[2 * j + 1] - (float)b[1])};
+          hi[j] = pack(b);
+          lo[j] = pack(r);
+        }
+      }
+      auto second = [&](const uint32_t (&v)[4][BF ? 4 : 8], const uint32_t (&v_lo)[4][BF ? 4 : 8], f32x4 (&o)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (BF) {
+            o[i] = mma(v_lo[i], lo, o[i]);
+            o[i] = mma(v[i], hi, o[i]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[i][j]), x[j], o[i], 0, 0, 0);
+          }
+        }
+      };
+      if constexpr (!CAREFUL) {
+        second(vt, vt, w.o);
+      } else {
+        // One query after the other, with the values of the keys that it does not see at zero; next to the weights' lower parts, whose sign is any,
+        // also those that are not finite.
+        for (int qn = 0; qn < 16; ++qn) {
+          const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)seen, qn) >> (4 * g);
+          uint32_t v[4][BF ? 4 : 8], v_lo[4][BF ? 4 : 8];
+#pragma unroll
+          for (int j = 0; j < (BF ? 4 : 8); ++j) {
+            uint32_t see;
+            if constexpr (BF) see = ((its >> (16 * (j >> 1) + 2 * (j & 1)) & 1) ? 0xffffu : 0u) | ((its >> (16 * (j >> 1) + 2 * (j & 1) + 1) & 1) ? 0xffff0000u : 0u);
+            else see = (its >> (16 * (j >> 2) + (j & 3)) & 1) ? ~0u : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              v[i][j] = vt[i][j] & see;
+              uint32_t fine = ~0u;
+              if constexpr (BF) fine = ((v[i][j] & 0x7f80u) != 0x7f80u ? 0xffffu : 0u) | ((v[i][j] & 0x7f800000u) != 0x7f800000u ? 0xffff0000u : 0u);
+              v_lo[i][j] = v[i][j] & fine;
+            }
+          }
+          f32x4 o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = w.o[i];
+          second(v, v_lo, o);
+          if (n16 == qn)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w.o[i] = o[i];
+        }
+      }
+    }
+  };
+  auto walk = [&](auto careful) {
+    reset();
+    if (t_first >= t_end) return;
+    Tile a, b;
+    int tile = t_first;
+    load(a, tile);
+    while (true) {
+      if (tile + NW < t_end) load(b, tile + NW);
+      compute(a, tile, careful);
+      if ((tile += NW) >= t_end) break;
+      if (tile + NW < t_end) load(a, tile + NW);
+      compute(b, tile, careful);
+      if ((tile += NW) >= t_end) break;
+    }
+  };
+  walk(std::false_type{});
+  // 0 x infinity and 0 x NaN of values that a row does not see (and infinity x the two parts of a weight) leave the result not finite, whatever follows.
+  // Then, and only then, the keys are walked again with every row's own values.
+  bool fine = true;
+#pragma unroll
+  for (int t = 0; t < NQ; ++t)
+    if (t * 16 + n16 < rows)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) fine = fine && is_finite(st[t].o[i][e]);
+  if (__ballot(!fine)) walk(std::true_type{});
+
+  // ---- the waves' parts meet
+  constexpr int kRow = 68;       // floats of a row in the LDS: 64 and room against bank conflicts
+  __shared__ float s_o[NW][16][kRow];
+  __shared__ float s_m[NW][16], s_l[NW][16];
+  const bool whole = p.n_split == 1 || n <= p.split_keys;      // no other workgroup has keys of this sequence
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    if (t > 0 && t >= n_tiles_q) break;
+    if (t > 0) __syncthreads();
+    const Pair rp = row_pair(st[t].l);
+    const float l = half_sum(rp.a + rp.b);
+    if (g == 0) { s_m[wave][n16] = st[t].m; s_l[wave][n16] = l; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(f32x4 *)&s_o[wave][n16][16 * g + 4 * i] = f32x4{st[t].o[0][i], st[t].o[1][i], st[t].o[2][i], st[t].o[3][i]};
+    __syncthreads();
+    for (int e = threadIdx.x; e < 256; e += 64 * NW) {
+      const int q = e >> 4, d = (e & 15) * 4;
+      float m = s_m[0][q];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) m = fmaxf(m, s_m[w][q]);
+      const float base = m == -INFINITY ? 0.0f : m;
+      f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+      float l_all = 0.0f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        if (s_l[w][q] == 0.0f) continue;                       // saw nothing
+        const float f = __builtin_amdgcn_exp2f(s_m[w][q] - base);
+        o += *(const f32x4 *)&s_o[w][q][d] * f;
+        l_all += s_l[w][q] * f;
+      }
+      const int local = t * 16 + q;
+      if (local >= rows) continue;
+      const int row = chunk * 16 * NQ + local;
+      if (whole) {
+        const float inv = l_all != 0.0f ? 1.0f / l_all : 0.0f;
+        o *= inv;
+        T *dst = (T *)p.out + (int64_t)(q_first + row / p.group) * p.ldo + (h * p.group + row % p.group) * 64 + d;
+        if constexpr (BF) *(bf16x4 *)dst = to_bf16x4(o);
+        else *(f32x4 *)dst = o;
+      } else {
+        const int64_t at = (((int64_t)s * H + h) * p.chunks * 16 * NQ + row) * p.n_split + z;
+        *(f32x4 *)(p.part + at * 64 + d) = o;
+        if (d == 0) { p.part_ml[2 * at] = m; p.part_ml[2 * at + 1] = l_all; }
+      }
+    }
+  }
+}
+
+// The parts of the rows whose keys several workgroups shared: 16 lanes a row.
+template <typename T>
+__global__ void __launch_bounds__(256) cache_attention_join_kernel(AttendArgs p, int rows_pad) {
+  const int64_t unit = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int d = (threadIdx.x & 15) * 4, H = p.c.n_heads;
+  const int64_t sh = unit / rows_pad;
+  if (sh >= (int64_t)p.n_seqs * H) return;
+  const int row = (int)(unit % rows_pad), s = (int)(sh / H), h = (int)(sh % H);
+  int q_first;
+  if (row >= sequence_queries(p, s, &q_first) * p.group) return;
+  int64_t row0;
+  const int n = sequence_keys(p, s, &row0);
+  if (n <= p.split_keys) return;
+  const int parts = (n + p.split_keys - 1) / p.split_keys;
+  const float *ml = p.part_ml + 2 * unit * p.n_split, *part = p.part + unit * p.n_split * 64 + d;
+  float m = -INFINITY;
+  for (int z = 0; z < parts; ++z) m = fmaxf(m, ml[2 * z]);
+  const float base = m == -INFINITY ? 0.0f : m;
+  f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+  float l = 0.0f;
+  for (int z = 0; z < parts; ++z) {
+    if (ml[2 * z + 1] == 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(ml[2 * z] - base);
+    o += *(const f32x4 *)(part + z * 64) * f;
+    l += ml[2 * z + 1] * f;
+  }
+  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+  o *= inv;
+  T *dst = (T *)p.out + (int64_t)(q_first + row / p.group) * p.ldo + (h * p.group + row % p.group) * 64 + d;
+  if constexpr (sizeof(T) == 2) *(bf16x4 *)dst = to_bf16x4(o);
+  else *(f32x4 *)dst = o;
+}
+
+struct Plan {
+  int nq, chunks, n_split, split_keys;
+};
+
+Plan plan_of(const wf_cache &c, const wf_cache_query &a) {
+  Plan p{};
+  const int64_t rows = (int64_t)std::min(a.max_q, std::max(a.n_q_rows, 1)) * (a.n_heads / c.n_heads);
+  p.nq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  p.chunks = (int)((rows + 16 * p.nq - 1) / (16 * p.nq));
+  const int64_t groups = (int64_t)a.n_seqs * c.n_heads * p.chunks, want = 1024;
+  int64_t n = groups >= want ? 1 : (want + groups - 1) / groups;
+  const int64_t most = std::max<int64_t>(1, a.max_len / 1024);
+  n = std::min<int64_t>(std::min(n, most), kMaxSplits);
+  p.split_keys = (int)std::min<int64_t>(host::round_up(std::max<int64_t>((a.max_len + n - 1) / n, kTile), kTile), INT32_MAX / kTile * kTile);
+  p.n_split = (int)std::max<int64_t>(1, ((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
+  return p;
+}
+
+template <typename T, int CACHE, int NQ, bool MASK>
+void launch_attend(const AttendArgs &p, dim3 grid, hipStream_t s) {
+  cache_attention_kernel<T, CACHE, NQ, 4, MASK><<<grid, 256, 0, s>>>(p);
+}
+
+template <typename T, int CACHE>
+void launch_attend(const AttendArgs &p, int nq, dim3 grid, hipStream_t s) {
+  if (p.mask) {
+    if (nq == 1) launch_attend<T, CACHE, 1, true>(p, grid, s);
+    else if (nq == 2) launch_attend<T, CACHE, 2, true>(p, grid, s);
+    else launch_attend<T, CACHE, 4, true>(p, grid, s);
+  } else {
+    if (nq == 1) launch_attend<T, CACHE, 1, false>(p, grid, s);
+    else if (nq == 2) launch_attend<T, CACHE, 2, false>(p, grid, s);
+    else launch_attend<T, CACHE, 4, false>(p, grid, s);
+  }
 }
 
 }  // namespace
@@ -98,16 +562,24 @@ int check_query(const wf_cache *c, const wf_cache_query *a) {
   if (a->n_seqs < 1 || a->n_q_rows < 0 || a->max_q < 1 || a->max_len < 0)
     return fail(WF_E_INVALID_ARG, "n_seqs = %d, n_q_rows = %d, max_q = %d, max_len = %d", a->n_seqs, a->n_q_rows, a->max_q, a->max_len);
   if (!std::isfinite(a->scale)) return fail(WF_E_INVALID_ARG, "scale is not finite");
-  if ((int64_t)a->n_seqs * std::min(a->max_q, std::max(a->n_q_rows, 1)) * a->n_heads >= ((int64_t)1 << 31))
-    return fail(WF_E_CAPACITY, "%d sequences of up to %d queries of %d heads: more than 2^31 rows", a->n_seqs, a->max_q, a->n_heads);
+  if ((double)a->n_seqs * std::min(a->max_q, std::max(a->n_q_rows, 1)) * a->n_heads >= (double)(1 << 30) || (double)a->n_seqs * c->n_heads >= (double)(1 << 24))
+    return fail(WF_E_CAPACITY, "%d sequences of up to %d queries of %d heads: more than 2^30 rows or 2^24 heads", a->n_seqs, a->max_q, a->n_heads);
   return WF_OK;
+}
+
+// Floats of the parts and of their maxima and sums.
+int64_t part_rows(const wf_cache &c, const wf_cache_query &a, const Plan &p) {
+  return p.n_split == 1 ? 0 : (int64_t)a.n_seqs * c.n_heads * p.chunks * 16 * p.nq * p.n_split;
 }
 
 }  // namespace
 
 extern "C" {
 
-int64_t wf_cache_attention_workspace(const wf_cache *cache, const wf_cache_query *query) { return check_query(cache, query); }
+int64_t wf_cache_attention_workspace(const wf_cache *cache, const wf_cache_query *query) {
+  const int rc = check_query(cache, query);
+  return rc ? rc : part_rows(*cache, *query, plan_of(*cache, *query)) * 66 * 4;
+}
 
 int wf_op_cache_attention(const wf_cache *cache, const wf_cache_query *query, void *hip_stream) {
   int rc = check_query(cache, query);
@@ -121,16 +593,29 @@ int wf_op_cache_attention(const wf_cache *cache, const wf_cache_query *query, vo
   if ((rc = check_cache_memory(cache))) return rc;
   if ((uintptr_t)a.q_dev % 16 || (uintptr_t)a.out_dev % 16 || a.ldq * es % 16 || a.ldo * es % 16)
     return fail(WF_E_INVALID_ARG, "q_dev, out_dev and their row strides must be multiples of 16 bytes");
-  const AttendArgs p{view_of(*cache), a.q_dev, a.out_dev, a.ldq, a.ldo, a.cu_q_dev, a.row_dev, a.len_dev, a.mask_dev, a.mask_from_dev,
-                     a.n_heads, a.n_seqs, a.n_q_rows, std::min(a.max_q, a.n_q_rows), a.max_len, a.mask_words, a.scale};
-  const dim3 grid((uint32_t)((int64_t)p.n_seqs * p.max_q * p.n_heads));
+  const Plan plan = plan_of(*cache, a);
+  const int64_t parts = part_rows(*cache, a, plan);
+  if (parts && (!a.workspace_dev || (uintptr_t)a.workspace_dev % 16)) return fail(WF_E_INVALID_ARG, "workspace_dev is NULL or not aligned to 16 bytes");
+  if (a.workspace_bytes < parts * 66 * 4) return fail(WF_E_CAPACITY, "workspace of %lld bytes, need %lld", (long long)a.workspace_bytes, (long long)parts * 66 * 4);
+  float *const part = (float *)a.workspace_dev;
+  const AttendArgs p{view_of(*cache), a.q_dev, a.out_dev, a.ldq, a.ldo, a.cu_q_dev, a.row_dev, a.len_dev, a.mask_dev, a.mask_from_dev, part, part + parts * 64,
+                     a.n_heads, a.n_heads / cache->n_heads, a.n_seqs, a.n_q_rows, a.max_q, a.max_len, a.mask_words, plan.chunks, plan.n_split, plan.split_keys, a.scale};
+  const int64_t groups = (int64_t)a.n_seqs * cache->n_heads * plan.chunks * plan.n_split;
+  if (groups >= (int64_t)1 << 31) return fail(WF_E_CAPACITY, "%lld workgroups", (long long)groups);
+  const dim3 grid((uint32_t)groups);
   const hipStream_t s = (hipStream_t)hip_stream;
   if (a.dtype == WF_DTYPE_BF16) {
-    if (cache->dtype == WF_DTYPE_F8) cache_attention_kernel<__bf16, WF_DTYPE_F8><<<grid, 64, 0, s>>>(p);
-    else cache_attention_kernel<__bf16, WF_DTYPE_BF16><<<grid, 64, 0, s>>>(p);
+    if (cache->dtype == WF_DTYPE_F8) launch_attend<__bf16, WF_DTYPE_F8>(p, plan.nq, grid, s);
+    else launch_attend<__bf16, WF_DTYPE_BF16>(p, plan.nq, grid, s);
   } else {
-    if (cache->dtype == WF_DTYPE_F8) cache_attention_kernel<float, WF_DTYPE_F8><<<grid, 64, 0, s>>>(p);
-    else cache_attention_kernel<float, WF_DTYPE_F32><<<grid, 64, 0, s>>>(p);
+    if (cache->dtype == WF_DTYPE_F8) launch_attend<float, WF_DTYPE_F8>(p, plan.nq, grid, s);
+    else launch_attend<float, WF_DTYPE_F32>(p, plan.nq, grid, s);
+  }
+  if (parts) {
+    const int rows_pad = plan.chunks * 16 * plan.nq;
+    const dim3 join((uint32_t)(((int64_t)a.n_seqs * cache->n_heads * rows_pad + 15) / 16));
+    if (a.dtype == WF_DTYPE_BF16) cache_attention_join_kernel<__bf16><<<join, 256, 0, s>>>(p, rows_pad);
+    else cache_attention_join_kernel<float><<<join, 256, 0, s>>>(p, rows_pad);
   }
   const hipError_t err = hipGetLastError();
   return err == hipSuccess ? WF_OK : fail(WF_E_HIP, "cache_attention launch: %s", hipGetErrorString(err));
