@@ -8,6 +8,8 @@ namespace wf {
 namespace {
 
 constexpr int kMaxBeams = 32;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Values as whole numbers of the same order (finite ones: > 0), so that (value, lowest token) is one comparison of 64 bits.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -19,27 +21,47 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ bool is_finite(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7f800000u) != 0x7f800000u; }
 
-__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
-  for (int m = 32; m; m >>= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)v, m);
-    v = v > o ? v : o;
-  }
-  return v;
+// Between a wave's writes to the LDS and its other lanes' reads: the LDS works in order, so only the compiler has to keep it.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Maxima over a wave by the same lane moves as device_utils.h's, on two registers.
+template <typename U, int N>
+__device__ __forceinline__ U row_rotate64(U v) {
+  const u32x2 u = __builtin_bit_cast(u32x2, v);
+  const uint32_t lo = u[0], hi = u[1];
+  const u32x2 r = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)lo, 0x120 + N, 0xF, 0xF, true), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)hi, 0x120 + N, 0xF, 0xF, true)};
+  return __builtin_bit_cast(U, r);
+}
+template <typename U>
+__device__ __forceinline__ U max64(U a, U b) { return a > b ? a : b; }
+template <typename U>
+__device__ __forceinline__ U wave_max64(U v) {
+  v = max64(v, row_rotate64<U, 8>(v));
+  v = max64(v, row_rotate64<U, 4>(v));
+  v = max64(v, row_rotate64<U, 2>(v));
+  v = max64(v, row_rotate64<U, 1>(v));
+  u32x2 u = __builtin_bit_cast(u32x2, v);
+  uint32_t lo = u[0], hi = u[1];
+  const auto l16 = __builtin_amdgcn_permlane16_swap(lo, lo, false, false), h16 = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+  const u32x2 a = {(uint32_t)l16[0], (uint32_t)h16[0]}, b = {(uint32_t)l16[1], (uint32_t)h16[1]};
+  u = __builtin_bit_cast(u32x2, max64(__builtin_bit_cast(U, a), __builtin_bit_cast(U, b)));
+  lo = u[0]; hi = u[1];
+  const auto l32 = __builtin_amdgcn_permlane32_swap(lo, lo, false, false), h32 = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+  const u32x2 c = {(uint32_t)l32[0], (uint32_t)h32[0]}, d = {(uint32_t)l32[1], (uint32_t)h32[1]};
+  return max64(__builtin_bit_cast(U, c), __builtin_bit_cast(U, d));
 }
 __device__ __forceinline__ double wave_sum_f64(double v) {
   for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
   return v;
 }
-__device__ __forceinline__ double wave_max_f64(double v) {
-  for (int m = 32; m; m >>= 1) v = fmax(v, __shfl_xor(v, m));
-  return v;
-}
 
-// What a beam offers: its candidates by logit and then the lowest token (token < 0: no more), and the log of its sum.
-struct RowBest {
-  double log_sum;
-  int32_t token[kMaxBeams];
-  float logit[kMaxBeams];
+// Part of a beam's row: the maximum and sum of its exponentials, and its best candidates as keys (0: no more).
+struct PartSum {
+  double sum;
+  float top, unused;
 };
 
 struct SelectArgs {
@@ -51,8 +73,9 @@ struct SelectArgs {
   int32_t *token_out, *parent_out;
   float *score_out;
   uint8_t *done_out;
-  RowBest *rows;
-  int32_t B, width, n_vocab, eos, keep_slots;
+  PartSum *sums;             // [beam][part]
+  uint64_t *keys;            // [beam][part][width]
+  int32_t B, width, n_vocab, eos, keep_slots, parts;
 };
 
 __device__ __forceinline__ int clamped(const int32_t *n, int s, int width) {
@@ -60,79 +83,194 @@ __device__ __forceinline__ int clamped(const int32_t *n, int s, int width) {
   return n[s] < 0 ? 0 : n[s] < width ? n[s] : width;
 }
 
-// One workgroup per beam.
+__device__ __forceinline__ uint64_t key_of(float x, int t) { return is_finite(x) ? (uint64_t)order_of(x) << 32 | (uint32_t)~t : 0; }
+
+constexpr int kPart = 2048;      // tokens of a part: 32 values a lane
+
+// A part's values as the lanes of its wave hold them: value e of chunk i is token first + i * 64 * N + lane * N + e, N = 16 bytes.  Rows start anywhere.
+template <typename T> struct Values;
+template <> struct Values<float> {
+  static constexpr int N = 4;
+  typedef float __attribute__((ext_vector_type(4), aligned(4))) vec;
+};
+template <> struct Values<__bf16> {
+  static constexpr int N = 8;
+  typedef __bf16 __attribute__((ext_vector_type(8), aligned(2))) vec;
+};
+
+// One wave per part: read once, into registers.  The width best are among the values that reach the width-th largest of the 64 lanes'
+// maxima (so many lanes do, each with one value at least); a bisection over the upper half of the bits finds a bound just below it,
+// usually a handful of values pass, and these are ranked by comparing each with each.  Where more than 64 pass (equal values, few finite
+// ones) the best are taken out one by one.
 template <typename T>
-__global__ void __launch_bounds__(256) beam_rows_kernel(SelectArgs p) {
-  const int s = blockIdx.x / p.width, b = blockIdx.x % p.width;
-  if (b >= clamped(p.n_in, s, p.width)) return;
-  RowBest &row = p.rows[blockIdx.x];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (p.done_in && p.done_in[blockIdx.x]) {
-    if (tid == 0) row.log_sum = 0.0;
-    if (tid < p.width) { row.token[tid] = tid == 0 ? p.eos : -1; row.logit[tid] = 0.0f; }
+__global__ void __launch_bounds__(256) beam_parts_kernel(SelectArgs p) {
+  constexpr int N = Values<T>::N, CH = 32 / N;
+  __shared__ uint64_t s_keys[4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+  const int row = (int)(id / p.parts), part = (int)(id % p.parts);
+  const int s = row / p.width, b = row % p.width;
+  if (s >= p.B || b >= clamped(p.n_in, s, p.width) || (p.done_in && p.done_in[row])) return;
+  const T *x = (const T *)p.logits + (int64_t)row * p.ld + (int64_t)part * kPart;
+  const int left = p.n_vocab - part * kPart;
+  float v[32];
+  if (left >= kPart) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const auto w = *(const typename Values<T>::vec *)(x + (i * 64 + lane) * N);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[i * N + e] = (float)w[e];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int at = (i * 64 + lane) * N + e;
+        v[i * N + e] = at < left ? (float)x[at] : -INFINITY;
+      }
+  }
+  float mine = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    v[i] = is_finite(v[i]) ? v[i] : -INFINITY;
+    mine = fmaxf(mine, v[i]);
+  }
+  const float top = wave_max(mine);
+  const int W = p.width;
+  uint64_t *keys = p.keys + id * W;
+  if (top == -INFINITY) {
+    if (lane < W) keys[lane] = 0;
+    if (lane == 0) p.sums[id] = PartSum{0.0, -INFINITY, 0.0f};
     return;
   }
-  __shared__ uint64_t best_of[4];
-  __shared__ double sum_of[4];
-  const T *x = (const T *)p.logits + (int64_t)blockIdx.x * p.ld;
-  uint64_t last = ~0ull;
-  for (int k = 0; k < p.width; ++k) {
-    uint64_t best = 0;
-    for (int t = tid; t < p.n_vocab; t += 256) {
-      const float v = (float)x[t];
-      const uint64_t key = is_finite(v) ? (uint64_t)order_of(v) << 32 | (uint32_t)~t : 0;
-      if (key < last && key > best) best = key;
+  // The sum: eight values in 32 bits, the rest in 64
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < 32; i += 8) {
+    float f = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f += __builtin_amdgcn_exp2f((v[i + e] - top) * 1.4426950408889634f);
+    sum += f;
+  }
+  sum = wave_sum_f64(sum);
+  if (lane == 0) p.sums[id] = PartSum{sum, top, 0.0f};
+
+  const uint32_t order = mine == -INFINITY ? 0 : order_of(mine);
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t higher = bound | 1u << bit;
+    if (__popcll(__ballot(order >= higher)) >= W) bound = higher;
+  }
+  const float least = bound > order_of(-3.4028234664e38f) ? value_of(bound) : -3.4028234664e38f;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const uint64_t who = __ballot(v[i] >= least);
+    if (!who) continue;
+    const int at = n + __popcll(who & ((1ull << lane) - 1));
+    if ((who >> lane & 1) && at < 64) s_keys[wave][at] = key_of(v[i], part * kPart + ((i / N) * 64 + lane) * N + i % N);
+    n += __popcll(who);
+  }
+  if (n <= 64) {
+    wave_sync();
+    const uint64_t key = lane < n ? s_keys[wave][lane] : 0;
+    const uint32_t lo = (uint32_t)key, hi = (uint32_t)(key >> 32);
+    int rank = 0;
+    for (int j = 0; j < n; ++j) {
+      const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)lo, j);
+      rank += other > key;
     }
-    best = wave_max_u64(best);
-    if (lane == 0) best_of[wave] = best;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) best = best > best_of[w] ? best : best_of[w];
-    __syncthreads();
-    if (tid == 0) { row.token[k] = best ? (int32_t)~(uint32_t)best : -1; row.logit[k] = best ? value_of((uint32_t)(best >> 32)) : 0.0f; }
-    if (k == 0 && best) {
-      const float top = value_of((uint32_t)(best >> 32));
-      double sum = 0.0;
-      for (int t = tid; t < p.n_vocab; t += 256) {
-        const float v = (float)x[t];
-        if (is_finite(v)) sum += expf(v - top);
+    if (lane < n && rank < W) keys[rank] = key;
+    if (lane >= n && lane < W) keys[lane] = 0;
+  } else {
+    uint64_t last = ~0ull;
+    for (int k = 0; k < W; ++k) {
+      uint64_t best = 0;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const uint64_t key = key_of(v[i], part * kPart + ((i / N) * 64 + lane) * N + i % N);
+        if (key < last && key > best) best = key;
       }
-      sum = wave_sum_f64(sum);
-      if (lane == 0) sum_of[wave] = sum;
-      __syncthreads();
-      if (tid == 0) row.log_sum = top + log(sum_of[0] + sum_of[1] + sum_of[2] + sum_of[3]);
+      last = wave_max64(best);
+      if (lane == 0) keys[k] = last;
     }
-    last = best;
   }
 }
 
-// One wave per stream: the beams' sorted candidates are merged, lane b holding the first of beam b that is not taken yet.
-__global__ void __launch_bounds__(64) beam_merge_kernel(SelectArgs p) {
+// One workgroup per stream.  A wave joins a beam's parts: the log of its sum, and the best of its parts' candidates.  Then the first wave merges the
+// beams' sorted candidates, lane b holding the first of beam b that is not taken yet.
+constexpr int kHeld = 4;      // keys of a beam that a lane keeps in registers
+__global__ void __launch_bounds__(512) beam_merge_kernel(SelectArgs p) {
+  __shared__ uint64_t s_key[kMaxBeams][kMaxBeams];
+  __shared__ double s_log[kMaxBeams];
   __shared__ int32_t s_token[kMaxBeams], s_parent[kMaxBeams], s_slot[kMaxBeams];
   __shared__ float s_score[kMaxBeams];
-  const int s = blockIdx.x, lane = threadIdx.x, W = p.width;
+  const int s = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, W = p.width;
   const int n_in = clamped(p.n_in, s, W), n_out = clamped(p.n_out, s, W);
-  const RowBest *row = p.rows + (int64_t)s * W + lane;
-  const float start = lane < n_in ? p.score_in[(int64_t)s * W + lane] : -INFINITY;
-  const bool live = lane < n_in && is_finite(start);
-  const bool was_done = live && p.done_in && p.done_in[(int64_t)s * W + lane];
-  int at = 0, token = live ? row->token[0] : -1;
-  double total = token >= 0 ? (double)start + ((double)row->logit[0] - row->log_sum) : -INFINITY;
-  int n = 0;
-  for (; n < n_out; ++n) {
-    const double best = wave_max_f64(total);
-    const uint64_t who = __ballot(token >= 0 && total == best);
-    if (!who) break;
-    const int b = __ffsll((unsigned long long)who) - 1;
-    if (lane == b) {
-      s_token[n] = was_done || token == p.eos ? token | 1 << 31 : token;       // the top bit: done
-      s_parent[n] = b;
-      s_score[n] = (float)total;
-      ++at;
-      token = at < W ? row->token[at] : -1;
-      total = token >= 0 ? (double)start + ((double)row->logit[at] - row->log_sum) : -INFINITY;
+  for (int b = wave; b < n_in; b += waves) {
+    const int64_t row = (int64_t)s * W + b;
+    if (p.done_in && p.done_in[row]) {
+      if (lane < W) s_key[b][lane] = lane == 0 ? key_of(0.0f, p.eos) : 0;
+      if (lane == 0) s_log[b] = 0.0;
+      continue;
+    }
+    const PartSum *sums = p.sums + row * p.parts;
+    const uint64_t *keys = p.keys + row * p.parts * W;
+    const int n = p.parts * W;
+    uint64_t held[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = lane + 64 * i < n ? keys[lane + 64 * i] : 0;
+    float top = -INFINITY;
+    for (int i = lane; i < p.parts; i += 64) top = fmaxf(top, sums[i].top);
+    top = wave_max(top);
+    double sum = 0.0;
+    for (int i = lane; i < p.parts; i += 64)
+      if (sums[i].top != -INFINITY) sum += sums[i].sum * exp((double)sums[i].top - (double)top);
+    sum = wave_sum_f64(sum);
+    if (lane == 0) s_log[b] = (double)top + log(sum);
+    uint64_t last = ~0ull;
+    for (int k = 0; k < W; ++k) {
+      uint64_t best = 0;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (held[i] < last && held[i] > best) best = held[i];
+      for (int i = lane + 64 * kHeld; i < n; i += 64) {
+        const uint64_t key = keys[i];
+        if (key < last && key > best) best = key;
+      }
+      last = wave_max64(best);
+      if (lane == 0) s_key[b][k] = last;
     }
   }
   __syncthreads();
+  if (wave > 0) return;
+  const float start = lane < n_in ? p.score_in[(int64_t)s * W + lane] : -INFINITY;
+  const bool live = lane < n_in && is_finite(start);
+  const bool was_done = live && p.done_in && p.done_in[(int64_t)s * W + lane];
+  const double log_sum = live ? s_log[lane] : 0.0;
+  int at = 0;
+  uint64_t key = live ? s_key[lane][0] : 0;
+  auto total_of = [&] { return key ? (double)start + ((double)value_of((uint32_t)(key >> 32)) - log_sum) : -(double)INFINITY; };
+  double total = total_of();
+  int n = 0;
+  for (; n < n_out; ++n) {
+    const double best = wave_max64(total);
+    const uint64_t who = __ballot(key != 0 && total == best);
+    if (!who) break;
+    const int b = __ffsll((unsigned long long)who) - 1;
+    if (lane == b) {
+      const int token = (int)~(uint32_t)key;
+      s_token[n] = was_done || token == p.eos ? token | (int)0x80000000 : token;       // the top bit: done
+      s_parent[n] = b;
+      s_score[n] = (float)total;
+      ++at;
+      key = at < W ? s_key[lane][at] : 0;
+      total = total_of();
+    }
+  }
+  wave_sync();
   if (lane == 0) {
     for (int j = 0; j < W; ++j) s_slot[j] = !p.keep_slots && j < n ? j : -1;
     if (p.keep_slots) {
@@ -147,7 +285,7 @@ __global__ void __launch_bounds__(64) beam_merge_kernel(SelectArgs p) {
       }
     }
   }
-  __syncthreads();
+  wave_sync();
   if (lane < W) {
     const int64_t o = (int64_t)s * W + lane;
     const int j = s_slot[lane];
@@ -207,6 +345,8 @@ using namespace wf::host;
 
 namespace {
 
+int parts_of(int32_t n_vocab) { return (int)(((int64_t)n_vocab + kPart - 1) / kPart); }
+
 int check_step(const wf_beam_step *a) {
   if (!a) return fail(WF_E_INVALID_ARG, "step is NULL");
   if (a->dtype != WF_DTYPE_F32 && a->dtype != WF_DTYPE_BF16) return fail(WF_E_INVALID_ARG, "logits dtype = %d", a->dtype);
@@ -214,6 +354,8 @@ int check_step(const wf_beam_step *a) {
   if (a->width < 1 || a->width > kMaxBeams) return fail(WF_E_INVALID_ARG, "width = %d (supported: 1 .. %d)", a->width, kMaxBeams);
   if (a->n_vocab < 1) return fail(WF_E_INVALID_ARG, "n_vocab = %d", a->n_vocab);
   if ((int64_t)a->B * a->width >= 1 << 22) return fail(WF_E_CAPACITY, "B * width = %lld beams (supported: below 2^22)", (long long)a->B * a->width);
+  if ((int64_t)a->B * a->width * parts_of(a->n_vocab) >= (int64_t)1 << 32)
+    return fail(WF_E_CAPACITY, "%d streams of %d beams over %d tokens: too many parts", a->B, a->width, a->n_vocab);
   return WF_OK;
 }
 
@@ -223,7 +365,7 @@ extern "C" {
 
 int64_t wf_beam_select_workspace(const wf_beam_step *a) {
   const int rc = check_step(a);
-  return rc ? rc : (int64_t)a->B * a->width * (int64_t)sizeof(RowBest);
+  return rc ? rc : (int64_t)a->B * a->width * parts_of(a->n_vocab) * (int64_t)(sizeof(PartSum) + 8 * a->width);
 }
 
 int wf_op_beam_select(const wf_beam_step *a, void *hip_stream) {
@@ -236,12 +378,16 @@ int wf_op_beam_select(const wf_beam_step *a, void *hip_stream) {
   if (a->done_in_dev && (a->eos < 0 || a->eos >= a->n_vocab)) return fail(WF_E_INVALID_ARG, "eos = %d outside [0, %d)", a->eos, a->n_vocab);
   if (!a->workspace_dev || (uintptr_t)a->workspace_dev % 16) return fail(WF_E_INVALID_ARG, "workspace_dev is NULL or not aligned to 16 bytes");
   if (a->workspace_bytes < need) return fail(WF_E_CAPACITY, "workspace of %lld bytes, need %lld", (long long)a->workspace_bytes, (long long)need);
+  const int parts = parts_of(a->n_vocab);
+  const int64_t waves = (int64_t)a->B * a->width * parts;
+  PartSum *const sums = (PartSum *)a->workspace_dev;
   const SelectArgs p{a->logits_dev, a->ld, a->n_in_dev, a->n_out_dev, a->score_in_dev, a->done_in_dev, a->token_out_dev, a->parent_out_dev, a->score_out_dev,
-                     a->done_out_dev, (RowBest *)a->workspace_dev, a->B, a->width, a->n_vocab, a->done_in_dev ? a->eos : -1, a->keep_slots};
+                     a->done_out_dev, sums, (uint64_t *)(sums + waves), a->B, a->width, a->n_vocab, a->done_in_dev ? a->eos : -1, a->keep_slots, parts};
   const hipStream_t s = (hipStream_t)hip_stream;
-  if (a->dtype == WF_DTYPE_BF16) beam_rows_kernel<__bf16><<<a->B * a->width, 256, 0, s>>>(p);
-  else beam_rows_kernel<float><<<a->B * a->width, 256, 0, s>>>(p);
-  beam_merge_kernel<<<a->B, 64, 0, s>>>(p);
+  const dim3 grid((uint32_t)((waves + 3) / 4));
+  if (a->dtype == WF_DTYPE_BF16) beam_parts_kernel<__bf16><<<grid, 256, 0, s>>>(p);
+  else beam_parts_kernel<float><<<grid, 256, 0, s>>>(p);
+  beam_merge_kernel<<<a->B, 64 * std::min(a->width, 8), 0, s>>>(p);
   const hipError_t err = hipGetLastError();
   return err == hipSuccess ? WF_OK : fail(WF_E_HIP, "beam_select launch: %s", hipGetErrorString(err));
 }
@@ -263,7 +409,7 @@ int wf_op_beam_reorder(void *dst_dev, const void *src_dev, const int32_t *parent
   if ((int64_t)n_layers * B * (double)p.chunks >= 2147483648.0) return fail(WF_E_CAPACITY, "%lld bytes in %d layers: more than 2^31 workgroups", (long long)all, n_layers);
   const int64_t ls = (int64_t)n_layers * B;
   const hipStream_t s = (hipStream_t)hip_stream;
-  if (vec == 16) launch_reorder<uint4>(p, ls, s);
+  if (vec == 16) launch_reorder<u32x4>(p, ls, s);
   else if (vec == 4) launch_reorder<uint32_t>(p, ls, s);
   else launch_reorder<uint8_t>(p, ls, s);
   const hipError_t err = hipGetLastError();
