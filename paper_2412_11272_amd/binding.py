@@ -722,49 +722,70 @@ def op_ln_linear(x, g, b, w, bias, out, epilogue: int, eps: float = 1e-5, stream
 
 
 # ---- token-by-token decoding: caches, attention over them, beams -------------------------------
-def _on_device(*tensors, dtype=None, what="tensor"):
-    """The tensors' common device is the current one (a launch goes to the current device's stream) and their type is `dtype`."""
+# (Called once per layer and token: a check is an attribute or two, and nothing is built that a launch does not need.)
+def _here(t, what: str) -> int:
+    """The device of a tensor, which has to be the current one: a launch goes to the current device's stream."""
     import torch
-    here = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda or t.device.index != here:
-            raise ValueError(f"{what} is on {t.device}, need the current CUDA device")
-        if dtype is not None and t.dtype != dtype:
-            raise TypeError(f"{what} is {t.dtype}, need {dtype}")
+    d = t.get_device()
+    if d < 0 or d != torch._C._cuda_getDevice():
+        raise ValueError(f"{what} is on {t.device}, need the current CUDA device")
+    return d
 
 
-def _index(t, n: int, what: str):
+def _stream_on(stream, here: int) -> int:
+    if stream is not None:
+        return stream
+    import torch
+    return torch._C._cuda_getCurrentRawStream(here)
+
+
+def _index(t, n: int, here: int, what: str):
     """Address of an int32 device array of n values (None: NULL)."""
     import torch
     if t is None:
         return None
-    _on_device(t, dtype=torch.int32, what=what)
-    if t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what}: {tuple(t.shape)}, need {n} contiguous values")
+    if t.get_device() != here or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {tuple(t.shape)} on {t.device}, need {n} contiguous values on the current CUDA device")
+    if t.dtype != torch.int32:
+        raise TypeError(f"{what} is {t.dtype}, need torch.int32")
     return t.data_ptr()
 
 
-def _rows_2d(t, what: str):
+def _rows_2d(t, here: int, what: str):
     """A matrix [rows, columns] whose rows are contiguous; a third dimension (heads, 64) is folded.  Returns (rows, columns, row stride)."""
-    _on_device(t, what=what)
-    if t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] <= 1 or t.stride(1) == t.shape[2]):
-        n, cols = t.shape[0], t.shape[1] * t.shape[2]
-    elif t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
-        n, cols = t.shape
+    shape, stride = t.shape, t.stride()
+    if t.get_device() != here:
+        raise ValueError(f"{what} is on {t.device}, need the current CUDA device")
+    if len(shape) == 2 and (stride[1] == 1 or shape[1] == 1):
+        n, cols = shape
+    elif len(shape) == 3 and stride[2] == 1 and (stride[1] == shape[2] or shape[1] <= 1):
+        n, cols = shape[0], shape[1] * shape[2]
     else:
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, strides {t.stride()}: need rows of contiguous values")
-    return n, cols, max(t.stride(0), cols) if n <= 1 else t.stride(0)
+        raise ValueError(f"{what}: shape {tuple(shape)}, strides {stride}: need rows of contiguous values")
+    return n, cols, stride[0] if n > 1 else cols
 
 
-def _empty(shape, dtype, device, stream):
+def _empty(shape, dtype, like, stream):
     """Uninitialised memory that belongs to the stream the call goes to (torch's allocator hands memory on in stream order)."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(torch.cuda.ExternalStream(stream)):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _fill_workspace(a, need: int, workspace, like, here: int, stream):
+    """Sets the call's workspace, its own where the caller gives none; the result has to live until the call is made."""
+    import torch
+    if need <= 0:
+        _check(need)
+        return None
+    if workspace is None:
+        workspace = _empty((need,), torch.uint8, like, stream)
+    elif workspace.get_device() != here or not workspace.is_contiguous():
+        raise ValueError("workspace: need contiguous memory on the current CUDA device")
+    a.workspace_dev, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace
 
 
 class Cache:
@@ -773,21 +794,18 @@ class Cache:
 
     def __init__(self, data, exps=None):
         import torch
+        shape = data.shape
         f8 = data.dtype == torch.float8_e4m3fn
-        code = WF_DTYPE_F8 if f8 else _torch_dtype_code(data.dtype)
-        _on_device(data, what="data")
-        if not data.is_contiguous() or data.dim() != (4 if f8 else 2) or (data.shape[2:] != (2, 64) if f8 else data.shape[1] % 128):
-            raise ValueError(f"data: {tuple(data.shape)} with strides {data.stride()}, need [n_rows, 128 n_heads] or, in 8 bits, [n_rows, n_heads, 2, 64]")
+        self.device = _here(data, "data")
+        if not data.is_contiguous() or (len(shape) != 4 or shape[2] != 2 or shape[3] != 64 if f8 else len(shape) != 2 or shape[1] % 128):
+            raise ValueError(f"data: {tuple(shape)} with strides {data.stride()}, need [n_rows, 128 n_heads] or, in 8 bits, [n_rows, n_heads, 2, 64]")
+        n_rows, n_heads = shape[0], shape[1] if f8 else shape[1] // 128
         if f8 != (exps is not None):
             raise ValueError("exps goes with float8_e4m3fn data and with no other")
-        self.n_rows, self.n_heads = data.shape[0], data.shape[1] if f8 else data.shape[1] // 128
-        if f8:
-            _on_device(exps, dtype=torch.uint8, what="exps")
-            if tuple(exps.shape) != (2 * self.n_heads, self.n_rows) or not exps.is_contiguous():
-                raise ValueError(f"exps: {tuple(exps.shape)}, need [{2 * self.n_heads}, {self.n_rows}]")
-        self.data, self.exps = data, exps
-        self._c = WfCache(data.data_ptr(), exps.data_ptr() if f8 else None, self.n_rows, self.n_heads, code)
-        self._at = C.addressof(self._c)
+        if f8 and (exps.dtype != torch.uint8 or exps.get_device() != self.device or exps.shape != (2 * n_heads, n_rows) or not exps.is_contiguous()):
+            raise ValueError(f"exps: {tuple(exps.shape)} {exps.dtype} on {exps.device}, need uint8 [{2 * n_heads}, {n_rows}] beside the data")
+        self.data, self.exps, self.n_rows, self.n_heads = data, exps, n_rows, n_heads
+        self._c = WfCache(data.data_ptr(), exps.data_ptr() if f8 else None, n_rows, n_heads, WF_DTYPE_F8 if f8 else _torch_dtype_code(data.dtype))
 
     @classmethod
     def empty(cls, n_rows: int, n_heads: int, dtype, device="cuda") -> "Cache":
@@ -802,26 +820,27 @@ class Cache:
 def op_cache_write(cache: Cache, k, v, cu, rows, stream=None) -> Cache:
     """Token t of sequence s (cu[s] <= t < cu[s + 1]) into cache row rows[s] + t - cu[s].  k, v: [n_tokens, 64 n_heads] or [n_tokens, n_heads,
     64], views into wider rows (a projection's output) with one row stride; cu [B + 1], rows [B]: int32 on the device."""
-    n, cols, ld = _rows_2d(k, "k")
-    if _rows_2d(v, "v") != (n, cols, ld) or v.dtype != k.dtype or cols != 64 * cache.n_heads:
+    here = _here(cache.data, "cache")
+    n, cols, ld = _rows_2d(k, here, "k")
+    if _rows_2d(v, here, "v") != (n, cols, ld) or v.dtype != k.dtype or cols != 64 * cache.n_heads:
         raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}: need two [n_tokens, {64 * cache.n_heads}] of one type and row stride")
     B = rows.numel()
-    _check(lib().wf_op_cache_write(cache._at, k.data_ptr(), v.data_ptr(), _torch_dtype_code(k.dtype), ld, _index(cu, B + 1, "cu"),
-                                   _index(rows, B, "rows"), B, n, _raw_stream(stream)))
+    _check(lib().wf_op_cache_write(C.byref(cache._c), k.data_ptr(), v.data_ptr(), _torch_dtype_code(k.dtype), ld, _index(cu, B + 1, here, "cu"),
+                                   _index(rows, B, here, "rows"), B, n, _stream_on(stream, here)))
     return cache
 
 
 def op_cache_read(cache: Cache, cu, rows, n_tokens: int, out=None, out_dtype=None, stream=None):
     """The rows op_cache_write fills, as [n_tokens, 128 n_heads] (keys of all heads, then values)."""
     import torch
+    here = _here(cache.data, "cache")
     if out is None:
-        out = _empty((n_tokens, 128 * cache.n_heads), out_dtype or torch.bfloat16, cache.data.device, stream)
-    _on_device(out, what="out")
-    if tuple(out.shape) != (n_tokens, 128 * cache.n_heads) or not out.is_contiguous():
-        raise ValueError(f"out: {tuple(out.shape)}, need a contiguous [{n_tokens}, {128 * cache.n_heads}]")
+        out = _empty((n_tokens, 128 * cache.n_heads), out_dtype or torch.bfloat16, cache.data, stream)
+    elif out.shape != (n_tokens, 128 * cache.n_heads) or not out.is_contiguous() or out.get_device() != here:
+        raise ValueError(f"out: {tuple(out.shape)} on {out.device}, need a contiguous [{n_tokens}, {128 * cache.n_heads}] beside the cache")
     B = rows.numel()
-    _check(lib().wf_op_cache_read(cache._at, _index(cu, B + 1, "cu"), _index(rows, B, "rows"), B, out.data_ptr(), _torch_dtype_code(out.dtype),
-                                  n_tokens, _raw_stream(stream)))
+    _check(lib().wf_op_cache_read(C.byref(cache._c), _index(cu, B + 1, here, "cu"), _index(rows, B, here, "rows"), B, out.data_ptr(),
+                                  _torch_dtype_code(out.dtype), n_tokens, _stream_on(stream, here)))
     return out
 
 
@@ -831,41 +850,30 @@ def op_cache_attention(cache: Cache, q, cu_q, rows, lens, max_q: int, max_len: i
     [n_q_rows, n_heads, 64]; cu_q [B + 1], rows, lens [B]: int32 on the device; max_q, max_len: upper bounds of a sequence's queries and keys.
     mask: int32 [n_q_rows, words], bit k - mask_from[s] (mask_from: int32 [B], None: 0) says whether a row sees key k; keys before
     mask_from[s] are seen by all."""
-    import torch
-    n, cols, ldq = _rows_2d(q, "q")
+    here = _here(cache.data, "cache")
+    n, cols, ldq = _rows_2d(q, here, "q")
     if cols % 64:
         raise ValueError(f"q: {cols} columns, need 64 for each head")
     if out is None:       # rows that belong to no sequence are not written
-        out = _empty(q.shape, q.dtype, q.device, stream)
-    n_out, cols_out, ldo = _rows_2d(out, "out")
-    if (n_out, cols_out) != (n, cols) or out.dtype != q.dtype:
-        raise ValueError(f"out: {tuple(out.shape)} {out.dtype}, need {tuple(q.shape)} {q.dtype}")
+        out, ldo = _empty(q.shape, q.dtype, q, stream), cols
+    else:
+        n_out, cols_out, ldo = _rows_2d(out, here, "out")
+        if n_out != n or cols_out != cols or out.dtype != q.dtype:
+            raise ValueError(f"out: {tuple(out.shape)} {out.dtype}, need {tuple(q.shape)} {q.dtype}")
     B = rows.numel()
-    words = 0
+    words, mask_at = 0, None
     if mask is not None:
-        _on_device(mask, dtype=torch.int32, what="mask")
-        if mask.dim() != 2 or mask.shape[0] != n or not mask.is_contiguous():
-            raise ValueError(f"mask: {tuple(mask.shape)}, need a contiguous [{n}, words]")
-        words = mask.shape[1]
-    a = WfCacheQuery(q.data_ptr(), out.data_ptr(), ldq, ldo, _index(cu_q, B + 1, "cu_q"), _index(rows, B, "rows"), _index(lens, B, "lens"),
-                     mask.data_ptr() if mask is not None else None, _index(mask_from, B, "mask_from"), None, 0, _torch_dtype_code(q.dtype),
+        words = mask.shape[-1]
+        if mask.dim() != 2:
+            raise ValueError(f"mask: {tuple(mask.shape)}, need [{n}, words]")
+        mask_at = _index(mask, n * words, here, "mask")
+    a = WfCacheQuery(q.data_ptr(), out.data_ptr(), ldq, ldo, _index(cu_q, B + 1, here, "cu_q"), _index(rows, B, here, "rows"),
+                     _index(lens, B, here, "lens"), mask_at, _index(mask_from, B, here, "mask_from"), None, 0, _torch_dtype_code(q.dtype),
                      cols // 64, B, n, max_q, max_len, words, scale)
-    at = C.addressof(a)
-    workspace = _fill_workspace(a, lib().wf_cache_attention_workspace(cache._at, at), workspace, q.device, stream)
-    _check(lib().wf_op_cache_attention(cache._at, at, _raw_stream(stream)))
+    L, c, at = lib(), C.byref(cache._c), C.byref(a)
+    workspace = _fill_workspace(a, L.wf_cache_attention_workspace(c, at), workspace, q, here, stream)
+    _check(L.wf_op_cache_attention(c, at, _stream_on(stream, here)))
     return out
-
-
-def _fill_workspace(a, need: int, workspace, device, stream):
-    """Sets the call's workspace, its own where the caller gives none; the result has to live until the call is made."""
-    import torch
-    _check(min(need, 0))
-    if workspace is None and need:
-        workspace = _empty(need, torch.uint8, device, stream)
-    if workspace is not None:
-        _on_device(workspace, what="workspace")
-        a.workspace_dev, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size() if workspace.is_contiguous() else 0
-    return workspace
 
 
 def op_beam_select(logits, scores, n_in=None, n_out=None, done=None, eos: int = -1, keep_slots: bool = False, workspace=None, stream=None):
@@ -873,50 +881,49 @@ def op_beam_select(logits, scores, n_in=None, n_out=None, done=None, eos: int = 
     [B] (None: width), done bool or uint8 [B, width] (None: no beam is done).  Returns (tokens, parents int32, scores float32, done or None),
     [B, width] each; keep_slots: a parent's best child stays in the parent's slot."""
     import torch
-    _on_device(logits, what="logits")
-    _on_device(scores, dtype=torch.float32, what="scores")
-    if logits.dim() != 3 or (logits.stride(2) != 1 and logits.shape[2] != 1):
-        raise ValueError(f"logits: {tuple(logits.shape)} with strides {logits.stride()}, need [B, width, n_vocab] with contiguous rows")
-    B, W, V = logits.shape
-    ld = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
-    if B > 1 and W > 1 and logits.stride(0) != W * ld:
-        raise ValueError(f"logits: strides {logits.stride()}, need one row stride over streams and beams")
+    here = _here(logits, "logits")
+    shape, stride = logits.shape, logits.stride()
+    if len(shape) != 3 or (stride[2] != 1 and shape[2] != 1):
+        raise ValueError(f"logits: {tuple(shape)} with strides {stride}, need [B, width, n_vocab] with contiguous rows")
+    B, W, V = shape
+    ld = stride[1] if W > 1 else stride[0] if B > 1 else V
+    if B > 1 and W > 1 and stride[0] != W * ld:
+        raise ValueError(f"logits: strides {stride}, need one row stride over streams and beams")
+    if scores.dtype != torch.float32 or (done is not None and done.dtype not in (torch.bool, torch.uint8)):
+        raise TypeError("need float32 scores and, if any, done of bool or uint8")
     for t in (scores, done):
-        if t is not None and (tuple(t.shape) != (B, W) or not t.is_contiguous()):
-            raise ValueError(f"scores, done: {tuple(t.shape)}, need a contiguous [{B}, {W}]")
+        if t is not None and (t.shape != (B, W) or t.get_device() != here or not t.is_contiguous()):
+            raise ValueError(f"scores, done: {tuple(t.shape)} on {t.device}, need a contiguous [{B}, {W}] beside the logits")
+    token, parent = _empty((B, W), torch.int32, scores, stream), _empty((B, W), torch.int32, scores, stream)
+    score, done_out = _empty((B, W), torch.float32, scores, stream), None
     if done is not None:
-        _on_device(done, what="done")
-        if done.dtype not in (torch.bool, torch.uint8):
-            raise TypeError(f"done is {done.dtype}, need bool or uint8")
-    dev = logits.device
-    token, parent = _empty((B, W), torch.int32, dev, stream), _empty((B, W), torch.int32, dev, stream)
-    score = _empty((B, W), torch.float32, dev, stream)
-    done_out = _empty((B, W), done.dtype, dev, stream) if done is not None else None
-    a = WfBeamStep(logits.data_ptr(), ld, _index(n_in, B, "n_in"), _index(n_out, B, "n_out"), scores.data_ptr(),
+        done_out = _empty((B, W), done.dtype, done, stream)
+    a = WfBeamStep(logits.data_ptr(), ld, _index(n_in, B, here, "n_in"), _index(n_out, B, here, "n_out"), scores.data_ptr(),
                    done.data_ptr() if done is not None else None, token.data_ptr(), parent.data_ptr(), score.data_ptr(),
                    done_out.data_ptr() if done is not None else None, None, 0, _torch_dtype_code(logits.dtype), B, W, V, eos, 1 if keep_slots else 0)
-    at = C.addressof(a)
-    workspace = _fill_workspace(a, lib().wf_beam_select_workspace(at), workspace, dev, stream)
-    _check(lib().wf_op_beam_select(at, _raw_stream(stream)))
+    L, at = lib(), C.byref(a)
+    workspace = _fill_workspace(a, L.wf_beam_select_workspace(at), workspace, scores, here, stream)
+    _check(L.wf_op_beam_select(at, _stream_on(stream, here)))
     return token, parent, score, done_out
 
 
 def op_beam_reorder(state, parents, lens=None, out=None, stream=None):
     """Slot (s, j) of every layer takes over slot (s, parents[s, j]).  state: contiguous [n_layers, B * width, n_pos, ..] of any type; parents int32
     [B, width]; lens int32 [B]: positions in use (None: all).  In place unless `out` is given."""
+    here = _here(state, "state")
+    shape, slots = state.shape, parents.numel()
+    if parents.dim() != 2 or len(shape) < 3 or shape[1] != slots:
+        raise ValueError(f"state: {tuple(shape)}, parents: {tuple(parents.shape)}: need [n_layers, B * width, n_pos, ..] and [B, width]")
     if out is None:
         out = state
-    _on_device(state, out, what="state")
-    if parents.dim() != 2 or state.dim() < 3 or state.shape[1] != parents.numel():
-        raise ValueError(f"state: {tuple(state.shape)}, parents: {tuple(parents.shape)}: need [n_layers, B * width, n_pos, ..] and [B, width]")
-    if not state.is_contiguous() or not out.is_contiguous() or out.shape != state.shape or out.dtype != state.dtype:
-        raise ValueError("state and out must be contiguous and of one shape and type")
+    if not state.is_contiguous() or (out is not state and (not out.is_contiguous() or out.shape != shape or out.dtype != state.dtype or out.get_device() != here)):
+        raise ValueError("state and out must be contiguous, of one shape and type and on one device")
+    if state.numel() == 0:
+        return out
     B, W = parents.shape
     pos_bytes = state.element_size()
-    for n in state.shape[3:]:
+    for n in shape[3:]:
         pos_bytes *= n
-    if pos_bytes == 0 or parents.numel() == 0:
-        return out
-    _check(lib().wf_op_beam_reorder(out.data_ptr(), state.data_ptr(), _index(parents, B * W, "parents"), _index(lens, B, "lens"), B, W,
-                                    state.shape[0], state.shape[2], pos_bytes, _raw_stream(stream)))
+    _check(lib().wf_op_beam_reorder(out.data_ptr(), state.data_ptr(), _index(parents, slots, here, "parents"), _index(lens, B, here, "lens"), B, W,
+                                    shape[0], shape[2], pos_bytes, _stream_on(stream, here)))
     return out
