@@ -17,13 +17,12 @@
 // What remains between loading V and multiplying is to pair two keys' values in a register: one byte permutation for two of them.
 //
 // Rounding: logits, statistics and sums are fp32.  Next to bf16 the weights enter as the sum of two bf16 parts (2^-17 of a weight is lost, where
-// one part would lose 2^-9): twice the second product's instructions, of which the kernel has plenty to spare.  The 8-bit caches' powers
-// of two multiply logits and weights, exactly.
+// one part would lose 2^-9): twice the second product's instructions, of which the kernel has plenty to spare.  Values of the 8-bit caches with their
+// powers of two are exact in either operand type.
 #include "cache_device.h"
 #include "host_runtime.h"
 
 #include <cmath>
-#include <type_traits>
 
 namespace wf {
 
@@ -80,7 +79,7 @@ template <int CACHE, int NQ, bool MASK>
 struct Tile {
   static constexpr int KD = 4 * Format<CACHE>::es, VD = Format<CACHE>::es;      // registers a key sub-tile, a value row
   uint32_t k[2][KD], v[8][VD];
-  uint32_t ke[CACHE == WF_DTYPE_F8 ? 2 : 1], ve[CACHE == WF_DTYPE_F8 ? 2 : 1];      // four exponents each
+  uint32_t ke[CACHE == WF_DTYPE_F8 ? 2 : 1], ve[CACHE == WF_DTYPE_F8 ? 2 : 1];      // exponents: of the lane's keys, of four of its value rows
   uint32_t word[MASK ? NQ : 1][2];
 };
 
@@ -101,13 +100,18 @@ __device__ __forceinline__ void load_dwords(uint32_t (&d)[N], const unsigned cha
 }
 
 __device__ __forceinline__ uint32_t pack(bf16x2 x) { return __builtin_bit_cast(uint32_t, x); }
-__device__ __forceinline__ uint32_t f8_pair(uint32_t x, bool high) {
-  return pack(high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
+// Two e4m3 values times a power of two, exactly; of `factor` only the exponent's bits 23 .. 30 count (0: 2^-127), whatever stands beside them.
+__device__ __forceinline__ uint32_t f8_pair(uint32_t x, uint32_t factor, bool high) {
+  const float f = __builtin_bit_cast(float, factor);
+  return pack(high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, f, false));
 }
-__device__ __forceinline__ float byte_value(uint32_t x, int i) {
-  return i == 0 ? __builtin_amdgcn_cvt_f32_fp8(x, 0) : i == 1 ? __builtin_amdgcn_cvt_f32_fp8(x, 1) : i == 2 ? __builtin_amdgcn_cvt_f32_fp8(x, 2)
-                                                                                               : __builtin_amdgcn_cvt_f32_fp8(x, 3);
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ f32x2 f8_pair_f32(uint32_t x, uint32_t factor, bool high) {
+  const float f = __builtin_bit_cast(float, factor);
+  return high ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, f, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, f, false);
 }
+// Byte i of four exponents where a factor has it
+__device__ __forceinline__ uint32_t exponent_of(uint32_t four, int i) { return i < 3 ? four << (23 - 8 * i) : four >> 1; }
 __device__ __forceinline__ bool is_finite(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7f800000u) != 0x7f800000u; }
 
 __device__ __forceinline__ f32x4 mma(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 c) {
@@ -121,17 +125,73 @@ struct State {
   f32x4 o[4];
 };
 
+// One row by one wave, 64 keys at a time, first a lane per key, then a lane per value: what a row does not see is not touched.
+struct RowState {
+  float m, l, o;
+};
+template <int CACHE>
+__device__ __forceinline__ float cache_value(const CacheView &c, int64_t r, int h, int kv, int i) {
+  if constexpr (CACHE == WF_DTYPE_F8)
+    return __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)c.data)[((r * c.n_heads + h) * 2 + kv) * 64 + i], 0) * f8_factor(c.exps[(2 * h + kv) * c.n_rows + r]);
+  else if constexpr (CACHE == WF_DTYPE_BF16)
+    return (float)((const __bf16 *)c.data)[(r * 2 + kv) * c.n_heads * 64 + h * 64 + i];
+  else
+    return ((const float *)c.data)[(r * 2 + kv) * c.n_heads * 64 + h * 64 + i];
+}
+template <typename T, int CACHE>
+__device__ __forceinline__ RowState one_row(const AttendArgs &p, int64_t r, int hq, int h, int64_t row0, int k_from, int k_to, int from) {
+  const int lane = threadIdx.x & 63;
+  const T *q = (const T *)p.q + r * p.ldq + hq * 64;
+  const float c = p.scale * 1.4426950408889634f;
+  RowState w{-INFINITY, 0.0f, 0.0f};
+#pragma unroll 1
+  for (int64_t k0 = k_from; k0 < k_to; k0 += 64) {
+    const int64_t k = k0 + lane;
+    bool seen = k < k_to;
+    if (seen && k >= from) {
+      const int64_t at = k - from;
+      seen = at < 32 * (int64_t)p.mask_words && (p.mask[r * p.mask_words + at / 32] >> (at & 31) & 1);
+    }
+    float x = -INFINITY;
+    if (seen) {
+      x = 0.0f;
+#pragma unroll 1
+      for (int d = 0; d < 64; ++d) x += (float)q[d] * cache_value<CACHE>(p.c, row0 + k, h, 0, d);
+      x *= c;
+    }
+    const uint64_t some = __ballot(seen);
+    if (!some) continue;
+    const float m = fmaxf(w.m, wave_max(x)), base = m == -INFINITY ? 0.0f : m;
+    const float e = seen ? __builtin_amdgcn_exp2f(x - base) : 0.0f, keep = __builtin_amdgcn_exp2f(w.m - base);
+    w.l = w.l * keep + wave_sum(e);
+    w.o *= keep;
+    w.m = m;
+#pragma unroll 1
+    for (int j = 0; j < 64; ++j)
+      if (some >> j & 1) w.o += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), j)) * cache_value<CACHE>(p.c, row0 + k0 + j, h, 1, lane);
+  }
+  return w;
+}
+
+template <typename T, int NQ>
+constexpr int min_waves() { return NQ == 1 && sizeof(T) == 2 ? 3 : 2; }
+
 template <typename T, int CACHE, int NQ, int NW, bool MASK>
-__global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) {
+__global__ void __launch_bounds__(64 * NW, (min_waves<T, NQ>())) cache_attention_kernel(AttendArgs p) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int es = Format<CACHE>::es;
   typedef Tile<CACHE, NQ, MASK> Tile;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
   const int H = p.c.n_heads;
-  int id = blockIdx.x;
+  // Workgroups go to the 8 XCDs in turn: those that read the same keys for other rows come 8 behind each other, to the same L2.
+  int id = blockIdx.x, chunk = 0;
+  if (p.chunks > 1) {
+    chunk = id / 8 % p.chunks;
+    id = id / (8 * p.chunks) * 8 + id % 8;
+  }
   const int h = id % H; id /= H;
-  const int s = id % p.n_seqs; id /= p.n_seqs;
-  const int chunk = id % p.chunks, z = id / p.chunks;
+  const int s = id % p.n_seqs, z = id / p.n_seqs;
+  if (z >= p.n_split) return;
 
   int q_first;
   const int rows = sequence_queries(p, s, &q_first) * p.group - chunk * 16 * NQ;      // of this chunk on
@@ -150,8 +210,10 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
   const uint8_t *k_exps = CACHE == WF_DTYPE_F8 ? p.c.exps + 2 * h * p.c.n_rows + row0 : nullptr;
   const uint8_t *v_exps = CACHE == WF_DTYPE_F8 ? k_exps + p.c.n_rows : nullptr;
 
-  // The lane's query of each of the 16-row tiles
-  uint32_t qr[NQ][BF ? 8 : 16];
+  // The lane's query of each of the 16-row tiles: in registers, or, for several tiles, in the LDS in the order the lanes read it
+  constexpr int QD = BF ? 8 : 16;
+  __shared__ u32x4 s_q[NQ > 1 ? NQ : 1][NQ > 1 ? QD / 4 : 1][64];
+  uint32_t q_one[QD];
   const uint32_t *words[MASK ? NQ : 1];
   (void)words;
 #pragma unroll
@@ -160,13 +222,20 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
     const bool have = local < rows;
     const int row = chunk * 16 * NQ + (have ? local : 0);
     const int64_t r = q_first + row / p.group;
-    const unsigned char *src = (const unsigned char *)p.q + (r * p.ldq + (h * p.group + row % p.group) * 64 + 16 * g) * sizeof(T);
-    load_dwords(qr[t], src, 0);
+    if constexpr (MASK) words[t] = p.mask + r * p.mask_words;
+    if (NQ > 1 && t % NW != wave) continue;
+    load_dwords(q_one, (const unsigned char *)p.q + (r * p.ldq + (h * p.group + row % p.group) * 64 + 16 * g) * sizeof(T), 0);
     if (!have)
 #pragma unroll
-      for (int i = 0; i < (BF ? 8 : 16); ++i) qr[t][i] = 0;
-    if constexpr (MASK) words[t] = p.mask + r * p.mask_words;
+      for (int i = 0; i < QD; ++i) q_one[i] = 0;
+    if (p.scale < 0.0f)               // so that the largest product is the largest logit
+#pragma unroll
+      for (int i = 0; i < QD; ++i) q_one[i] ^= BF ? 0x80008000u : 0x80000000u;
+    if constexpr (NQ > 1)
+#pragma unroll
+      for (int i = 0; i < QD / 4; ++i) s_q[t][i][lane] = u32x4{q_one[4 * i], q_one[4 * i + 1], q_one[4 * i + 2], q_one[4 * i + 3]};
   }
+  if constexpr (NQ > 1) __syncthreads();
   const int from = MASK && p.mask_from ? p.mask_from[s] : 0;
 
   const uint32_t k_lane = n16 * row_bytes + g * 16 * es, v_lane = 4 * g * row_bytes + v_off + n16 * 4 * es;
@@ -181,7 +250,7 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
       if constexpr (CACHE == WF_DTYPE_F8)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          __builtin_memcpy(&a.ke[u], k_exps + tile * kTile + 16 * u + 4 * g, 4);
+          a.ke[u] = k_exps[tile * kTile + 16 * u + n16];
           __builtin_memcpy(&a.ve[u], v_exps + tile * kTile + 16 * u + 4 * g, 4);
         }
     } else {                          // keys behind the last are the last again, their values are zero
@@ -201,12 +270,12 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
       if constexpr (CACHE == WF_DTYPE_F8)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          a.ke[u] = a.ve[u] = 0;
+          a.ke[u] = k_exps[tile * kTile + (16 * u + n16 < left ? 16 * u + n16 : left - 1)];
+          a.ve[u] = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int key = 16 * u + 4 * g + i, at = tile * kTile + (key < left ? key : left - 1);
-            a.ke[u] |= (uint32_t)k_exps[at] << (8 * i);
-            a.ve[u] |= (uint32_t)v_exps[at] << (8 * i);
+            const int key = 16 * u + 4 * g + i;
+            a.ve[u] |= (uint32_t)v_exps[tile * kTile + (key < left ? key : left - 1)] << (8 * i);
           }
         }
     }
@@ -233,66 +302,81 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
   };
 
   State st[NQ];
-  const float c = p.scale * 1.4426950408889634f;      // exp(s scale) = exp2(s c)
-  auto reset = [&] {
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      st[t].m = -INFINITY;
-      st[t].l = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) st[t].o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-  };
+  const float c = fabsf(p.scale) * 1.4426950408889634f;      // exp(s scale) = exp2(s c)
 
-  auto compute = [&](const Tile &a, int tile, auto careful) {
-    constexpr bool CAREFUL = decltype(careful)::value;
+  auto compute = [&](const Tile &a, int tile) {
     // ---- values: pairs of keys next to each other
     uint32_t vt[4][BF ? 4 : 8];
     if constexpr (BF) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (CACHE == WF_DTYPE_F8) {
-          const uint32_t x = __builtin_amdgcn_perm(a.v[2 * j + 1][0], a.v[2 * j][0], 0x05010400), y = __builtin_amdgcn_perm(a.v[2 * j + 1][0], a.v[2 * j][0], 0x07030602);
-          vt[0][j] = f8_pair(x, false); vt[1][j] = f8_pair(x, true);
-          vt[2][j] = f8_pair(y, false); vt[3][j] = f8_pair(y, true);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            vt[2 * i][j] = __builtin_amdgcn_perm(a.v[2 * j + 1][i], a.v[2 * j][i], 0x05040100);
-            vt[2 * i + 1][j] = __builtin_amdgcn_perm(a.v[2 * j + 1][i], a.v[2 * j][i], 0x07060302);
-          }
-        }
-      }
-    } else {
+      uint32_t v[8][2];
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          if constexpr (CACHE == WF_DTYPE_F8) vt[t][j] = __builtin_bit_cast(uint32_t, byte_value(a.v[j][0], t));
-          else vt[t][j] = a.v[j][t];
+        for (int i = 0; i < 2; ++i) {
+          if constexpr (CACHE == WF_DTYPE_F8) v[j][i] = f8_pair(a.v[j][0], exponent_of(a.ve[j >> 2], j & 3), i == 1);
+          else v[j][i] = a.v[j][i];
         }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          vt[2 * i][j] = __builtin_amdgcn_perm(v[2 * j + 1][i], v[2 * j][i], 0x05040100);
+          vt[2 * i + 1][j] = __builtin_amdgcn_perm(v[2 * j + 1][i], v[2 * j][i], 0x07060302);
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (CACHE == WF_DTYPE_F8) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const f32x2 x = f8_pair_f32(a.v[j][0], exponent_of(a.ve[j >> 2], j & 3), i == 1);
+            const float x0 = x[0], x1 = x[1];
+            vt[2 * i][j] = __builtin_bit_cast(uint32_t, x0);
+            vt[2 * i + 1][j] = __builtin_bit_cast(uint32_t, x1);
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) vt[t][j] = a.v[j][t];
+        }
+      }
     }
     // ---- keys
-    uint32_t kt[2][BF ? 8 : 16];
+    uint32_t kt[2][QD];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if constexpr (CACHE == WF_DTYPE_F8) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (BF) { kt[u][2 * i] = f8_pair(a.k[u][i], false); kt[u][2 * i + 1] = f8_pair(a.k[u][i], true); }
-          else
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) kt[u][4 * i + b] = __builtin_bit_cast(uint32_t, byte_value(a.k[u][i], b));
-        }
+          for (int e = 0; e < 2; ++e) {
+            if constexpr (BF) {
+              kt[u][2 * i + e] = f8_pair(a.k[u][i], a.ke[u] << 23, e == 1);
+            } else {
+              const f32x2 x = f8_pair_f32(a.k[u][i], a.ke[u] << 23, e == 1);
+              const float x0 = x[0], x1 = x[1];
+              kt[u][4 * i + 2 * e] = __builtin_bit_cast(uint32_t, x0);
+              kt[u][4 * i + 2 * e + 1] = __builtin_bit_cast(uint32_t, x1);
+            }
+          }
       } else {
 #pragma unroll
-        for (int i = 0; i < (BF ? 8 : 16); ++i) kt[u][i] = a.k[u][i];
+        for (int i = 0; i < QD; ++i) kt[u][i] = a.k[u][i];
       }
     }
+    const bool whole_tile = n - tile * kTile >= kTile && (!MASK || (int64_t)(tile + 1) * kTile <= from);      // every row sees every key
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
       if (t > 0 && t >= n_tiles_q) break;
       State &w = st[t];
+      uint32_t qa[QD];
+#pragma unroll
+      for (int i = 0; i < QD; ++i) qa[i] = q_one[i];
+      if constexpr (NQ > 1)
+#pragma unroll
+        for (int i = 0; i < QD / 4; ++i) {
+          const u32x4 x = s_q[t][i][lane];
+          qa[4 * i] = x[0]; qa[4 * i + 1] = x[1]; qa[4 * i + 2] = x[2]; qa[4 * i + 3] = x[3];
+        }
       float x[8];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -301,22 +385,19 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
 #pragma unroll
           for (int f = 0; f < 2; ++f) {
             const uint32_t ka[4] = {kt[u][4 * f], kt[u][4 * f + 1], kt[u][4 * f + 2], kt[u][4 * f + 3]};
-            const uint32_t qa[4] = {qr[t][4 * f], qr[t][4 * f + 1], qr[t][4 * f + 2], qr[t][4 * f + 3]};
-            d = mma(ka, qa, d);
+            const uint32_t qb[4] = {qa[4 * f], qa[4 * f + 1], qa[4 * f + 2], qa[4 * f + 3]};
+            d = mma(ka, qb, d);
           }
         } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            d = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kt[u][i]), __builtin_bit_cast(float, qr[t][i]), d, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kt[u][i]), __builtin_bit_cast(float, qa[i]), d, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[4 * u + i] = d[i] * c;
-          if constexpr (CACHE == WF_DTYPE_F8) x[4 * u + i] *= f8_factor((a.ke[u] >> (8 * i)) & 0xff);
-        }
+        for (int i = 0; i < 4; ++i) x[4 * u + i] = d[i];
       }
       uint32_t seen = ~0u;
-      if (MASK || CAREFUL || n - tile * kTile < kTile) {
+      if (!whole_tile) {
         seen = seen_keys(a, tile, t);
         const uint32_t mine = seen >> (4 * g);
 #pragma unroll
@@ -327,21 +408,23 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
 #pragma unroll
       for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
       const Pair rp = row_pair(top);
-      top = fmaxf(w.m, half_max(fmaxf(rp.a, rp.b)));
-      if (__ballot(top > w.m)) {
+      top = half_max(fmaxf(rp.a, rp.b));
+      top = top == -INFINITY ? top : top * c;
+      // The reference follows the maximum only where that is 2^8 above it: weights of up to 2^8 lose nothing in fp32.
+      if (__ballot(top > w.m + 8.0f)) {
+        top = fmaxf(top, w.m);
         const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - top);
         w.l *= keep;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w.o[i] *= keep;
         w.m = top;
       }
-      const float base = top == -INFINITY ? 0.0f : top;
+      const float base = w.m == -INFINITY ? 0.0f : w.m;
       float sum = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        x[j] = __builtin_amdgcn_exp2f(x[j] - base);
+        x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], c, -base));
         sum += x[j];
-        if constexpr (CACHE == WF_DTYPE_F8) x[j] *= f8_factor((a.ve[j >> 2] >> (8 * (j & 3))) & 0xff);
       }
       w.l += sum;
       uint32_t hi[4], lo[4];
@@ -354,83 +437,81 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
           lo[j] = pack(r);
         }
       }
-      auto second = [&](const uint32_t (&v)[4][BF ? 4 : 8], const uint32_t (&v_lo)[4][BF ? 4 : 8], f32x4 (&o)[4]) {
+      auto second = [&](const uint32_t (&v)[BF ? 4 : 8], const uint32_t (&v_lo)[BF ? 4 : 8], f32x4 o) -> f32x4 {
+        if constexpr (BF) {
+          return mma(v, hi, mma(v_lo, lo, o));
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (BF) {
-            o[i] = mma(v_lo[i], lo, o[i]);
-            o[i] = mma(v[i], hi, o[i]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[i][j]), x[j], o[i], 0, 0, 0);
-          }
+          for (int j = 0; j < 8; ++j) o = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[j]), x[j], o, 0, 0, 0);
+          return o;
         }
       };
-      if constexpr (!CAREFUL) {
-        second(vt, vt, w.o);
-      } else {
-        // One query after the other, with the values of the keys that it does not see at zero; next to the weights' lower parts, whose sign is any,
-        // also those that are not finite.
-        for (int qn = 0; qn < 16; ++qn) {
-          const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)seen, qn) >> (4 * g);
-          uint32_t v[4][BF ? 4 : 8], v_lo[4][BF ? 4 : 8];
 #pragma unroll
-          for (int j = 0; j < (BF ? 4 : 8); ++j) {
-            uint32_t see;
-            if constexpr (BF) see = ((its >> (16 * (j >> 1) + 2 * (j & 1)) & 1) ? 0xffffu : 0u) | ((its >> (16 * (j >> 1) + 2 * (j & 1) + 1) & 1) ? 0xffff0000u : 0u);
-            else see = (its >> (16 * (j >> 2) + (j & 3)) & 1) ? ~0u : 0u;
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (BF) {
+          w.o[i] = mma(vt[i], hi, mma(vt[i], lo, w.o[i]));
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              v[i][j] = vt[i][j] & see;
-              uint32_t fine = ~0u;
-              if constexpr (BF) fine = ((v[i][j] & 0x7f80u) != 0x7f80u ? 0xffffu : 0u) | ((v[i][j] & 0x7f800000u) != 0x7f800000u ? 0xffff0000u : 0u);
-              v_lo[i][j] = v[i][j] & fine;
-            }
-          }
-          f32x4 o[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[i] = w.o[i];
-          second(v, v_lo, o);
-          if (n16 == qn)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w.o[i] = o[i];
+          for (int j = 0; j < 8; ++j) w.o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vt[i][j]), x[j], w.o[i], 0, 0, 0);
         }
       }
     }
   };
-  auto walk = [&](auto careful) {
-    reset();
-    if (t_first >= t_end) return;
-    Tile a, b;
-    int tile = t_first;
-    load(a, tile);
-    while (true) {
-      if (tile + NW < t_end) load(b, tile + NW);
-      compute(a, tile, careful);
-      if ((tile += NW) >= t_end) break;
-      if (tile + NW < t_end) load(a, tile + NW);
-      compute(b, tile, careful);
-      if ((tile += NW) >= t_end) break;
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    st[t].m = -INFINITY;
+    st[t].l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) st[t].o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  int tile = t_first;
+  Tile a, b;
+  if (tile < t_end) load(a, tile);
+  while (tile < t_end) {
+    if (tile + NW < t_end) load(b, tile + NW);
+    compute(a, tile);
+    if ((tile += NW) >= t_end) break;
+    if (tile + NW < t_end) load(a, tile + NW);
+    compute(b, tile);
+    tile += NW;
+  }
+  const bool whole = p.n_split == 1 || n <= p.split_keys;      // no other workgroup has keys of this sequence
+  const int64_t part_at = (((int64_t)s * H + h) * p.chunks + chunk) * 16 * NQ * p.n_split + z;      // of row 0 of the chunk; a row on: n_split
+
+  // 0 x infinity and 0 x NaN of values that a row does not see, and infinity x the two parts of a weight, leave the result not finite, whatever
+  // follows.  Then, and only then, the rows are computed one by one.
+  if constexpr (BF || MASK) {
+    bool fine = true;
+#pragma unroll
+    for (int t = 0; t < NQ; ++t)
+      if (t * 16 + n16 < rows)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) fine = fine && is_finite(st[t].o[i][e]);
+    if (__syncthreads_or(!fine)) {
+      const int to = (int)(split_from + p.split_keys < n ? split_from + p.split_keys : n);
+      for (int local = wave; local < rows && local < 16 * NQ; local += NW) {
+        const int row = chunk * 16 * NQ + local;
+        const int64_t r = q_first + row / p.group;
+        const int hq = h * p.group + row % p.group;
+        const RowState w = one_row<T, CACHE>(p, r, hq, h, row0, (int)split_from, to, MASK ? from : INT32_MAX);
+        if (whole) {
+          ((T *)p.out)[r * p.ldo + hq * 64 + lane] = (T)(w.l != 0.0f ? w.o / w.l : 0.0f);
+        } else {
+          const int64_t at = part_at + (int64_t)local * p.n_split;
+          p.part[at * 64 + lane] = w.o;
+          if (lane == 0) { p.part_ml[2 * at] = w.m; p.part_ml[2 * at + 1] = w.l; }
+        }
+      }
+      return;
     }
-  };
-  walk(std::false_type{});
-  // 0 x infinity and 0 x NaN of values that a row does not see (and infinity x the two parts of a weight) leave the result not finite, whatever follows.
-  // Then, and only then, the keys are walked again with every row's own values.
-  bool fine = true;
-#pragma unroll
-  for (int t = 0; t < NQ; ++t)
-    if (t * 16 + n16 < rows)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) fine = fine && is_finite(st[t].o[i][e]);
-  if (__ballot(!fine)) walk(std::true_type{});
+  }
 
   // ---- the waves' parts meet
   constexpr int kRow = 68;       // floats of a row in the LDS: 64 and room against bank conflicts
   __shared__ float s_o[NW][16][kRow];
   __shared__ float s_m[NW][16], s_l[NW][16];
-  const bool whole = p.n_split == 1 || n <= p.split_keys;      // no other workgroup has keys of this sequence
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
     if (t > 0 && t >= n_tiles_q) break;
@@ -466,7 +547,7 @@ __global__ void __launch_bounds__(64 * NW) cache_attention_kernel(AttendArgs p) 
         if constexpr (BF) *(bf16x4 *)dst = to_bf16x4(o);
         else *(f32x4 *)dst = o;
       } else {
-        const int64_t at = (((int64_t)s * H + h) * p.chunks * 16 * NQ + row) * p.n_split + z;
+        const int64_t at = part_at + (int64_t)local * p.n_split;
         *(f32x4 *)(p.part + at * 64 + d) = o;
         if (d == 0) { p.part_ml[2 * at] = m; p.part_ml[2 * at + 1] = l_all; }
       }
@@ -514,7 +595,7 @@ struct Plan {
 Plan plan_of(const wf_cache &c, const wf_cache_query &a) {
   Plan p{};
   const int64_t rows = (int64_t)std::min(a.max_q, std::max(a.n_q_rows, 1)) * (a.n_heads / c.n_heads);
-  p.nq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  p.nq = rows <= 16 ? 1 : rows <= 32 || a.dtype == WF_DTYPE_F32 ? 2 : 4;      // 64 rows of fp32 operands outgrow the registers
   p.chunks = (int)((rows + 16 * p.nq - 1) / (16 * p.nq));
   const int64_t groups = (int64_t)a.n_seqs * c.n_heads * p.chunks, want = 1024;
   int64_t n = groups >= want ? 1 : (want + groups - 1) / groups;
@@ -535,11 +616,11 @@ void launch_attend(const AttendArgs &p, int nq, dim3 grid, hipStream_t s) {
   if (p.mask) {
     if (nq == 1) launch_attend<T, CACHE, 1, true>(p, grid, s);
     else if (nq == 2) launch_attend<T, CACHE, 2, true>(p, grid, s);
-    else launch_attend<T, CACHE, 4, true>(p, grid, s);
+    else if constexpr (sizeof(T) == 2) launch_attend<T, CACHE, 4, true>(p, grid, s);
   } else {
     if (nq == 1) launch_attend<T, CACHE, 1, false>(p, grid, s);
     else if (nq == 2) launch_attend<T, CACHE, 2, false>(p, grid, s);
-    else launch_attend<T, CACHE, 4, false>(p, grid, s);
+    else if constexpr (sizeof(T) == 2) launch_attend<T, CACHE, 4, false>(p, grid, s);
   }
 }
 
@@ -600,7 +681,8 @@ int wf_op_cache_attention(const wf_cache *cache, const wf_cache_query *query, vo
   float *const part = (float *)a.workspace_dev;
   const AttendArgs p{view_of(*cache), a.q_dev, a.out_dev, a.ldq, a.ldo, a.cu_q_dev, a.row_dev, a.len_dev, a.mask_dev, a.mask_from_dev, part, part + parts * 64,
                      a.n_heads, a.n_heads / cache->n_heads, a.n_seqs, a.n_q_rows, a.max_q, a.max_len, a.mask_words, plan.chunks, plan.n_split, plan.split_keys, a.scale};
-  const int64_t groups = (int64_t)a.n_seqs * cache->n_heads * plan.chunks * plan.n_split;
+  int64_t groups = (int64_t)a.n_seqs * cache->n_heads * plan.n_split;
+  if (plan.chunks > 1) groups = round_up(groups, 8) * plan.chunks;
   if (groups >= (int64_t)1 << 31) return fail(WF_E_CAPACITY, "%lld workgroups", (long long)groups);
   const dim3 grid((uint32_t)groups);
   const hipStream_t s = (hipStream_t)hip_stream;
