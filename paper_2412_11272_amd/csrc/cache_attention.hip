@@ -31,6 +31,7 @@ namespace {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 32;      // keys
 constexpr int kMaxSplits = 64;
@@ -83,19 +84,28 @@ struct Tile {
   uint32_t word[MASK ? NQ : 1][2];
 };
 
+// N registers from `at` bytes on: of memory, or of a buffer (zero past its end).
 template <int N>
 __device__ __forceinline__ void load_dwords(uint32_t (&d)[N], const unsigned char *base, uint32_t at) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const u32x4 x = *(const u32x4 *)(base + at + 4 * i);
+    d[i] = x[0]; d[i + 1] = x[1]; d[i + 2] = x[2]; d[i + 3] = x[3];
+  }
+}
+template <int N>
+__device__ __forceinline__ void load_dwords(uint32_t (&d)[N], __amdgpu_buffer_rsrc_t base, uint32_t at) {
   if constexpr (N >= 4) {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-      const u32x4 x = *(const u32x4 *)(base + at + 4 * i);
+      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(base, at + 4 * i, 0, 0);
       d[i] = x[0]; d[i + 1] = x[1]; d[i + 2] = x[2]; d[i + 3] = x[3];
     }
   } else if constexpr (N == 2) {
-    const u32x2 x = *(const u32x2 *)(base + at);
+    const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(base, at, 0, 0);
     d[0] = x[0]; d[1] = x[1];
   } else {
-    d[0] = *(const uint32_t *)(base + at);
+    d[0] = __builtin_amdgcn_raw_buffer_load_b32(base, at, 0, 0);
   }
 }
 
@@ -105,7 +115,6 @@ __device__ __forceinline__ uint32_t f8_pair(uint32_t x, uint32_t factor, bool hi
   const float f = __builtin_bit_cast(float, factor);
   return pack(high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, f, false));
 }
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ f32x2 f8_pair_f32(uint32_t x, uint32_t factor, bool high) {
   const float f = __builtin_bit_cast(float, factor);
   return high ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, f, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, f, false);
@@ -173,11 +182,11 @@ __device__ __forceinline__ RowState one_row(const AttendArgs &p, int64_t r, int 
   return w;
 }
 
-template <typename T, int NQ>
-constexpr int min_waves() { return NQ == 1 && sizeof(T) == 2 ? 3 : 2; }
+template <typename T, int CACHE, int NQ, bool MASK>
+constexpr int min_waves() { return NQ == 1 && sizeof(T) == 2 ? CACHE == WF_DTYPE_F8 && !MASK ? 3 : 3 : 2; }
 
 template <typename T, int CACHE, int NQ, int NW, bool MASK>
-__global__ void __launch_bounds__(64 * NW, (min_waves<T, NQ>())) cache_attention_kernel(AttendArgs p) {
+__global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) cache_attention_kernel(AttendArgs p) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int es = Format<CACHE>::es;
   typedef Tile<CACHE, NQ, MASK> Tile;
@@ -238,46 +247,36 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, NQ>())) cache_attention
   if constexpr (NQ > 1) __syncthreads();
   const int from = MASK && p.mask_from ? p.mask_from[s] : 0;
 
+  // Sub-tiles of 16 keys go through buffers that end behind the sequence's last key: rows past it read as zero.
   const uint32_t k_lane = n16 * row_bytes + g * 16 * es, v_lane = 4 * g * row_bytes + v_off + n16 * 4 * es;
   auto load = [&](Tile &a, int tile) {
-    const unsigned char *base = seq + (int64_t)tile * kTile * row_bytes;
     const int left = n - tile * kTile;
-    if (left >= kTile) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) load_dwords(a.k[u], base + 16 * u * row_bytes, k_lane);
+    for (int u = 0; u < 2; ++u) {
+      const int keys = left - 16 * u < 16 ? left - 16 * u : 16;
+      const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void *)(seq + ((int64_t)tile * kTile + 16 * u) * row_bytes), 0,
+                                                            keys > 0 ? (keys - 1) * row_bytes + v_off + 64 * es : 0, 0x00027000);
+      load_dwords(a.k[u], buffer, k_lane);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) load_dwords(a.v[j], base + (16 * (j >> 2) + (j & 3)) * row_bytes, v_lane);
-      if constexpr (CACHE == WF_DTYPE_F8)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          a.ke[u] = k_exps[tile * kTile + 16 * u + n16];
-          __builtin_memcpy(&a.ve[u], v_exps + tile * kTile + 16 * u + 4 * g, 4);
-        }
-    } else {                          // keys behind the last are the last again, their values are zero
+      for (int j = 0; j < 4; ++j) load_dwords(a.v[4 * u + j], buffer, v_lane + j * row_bytes);
+    }
+    if constexpr (CACHE == WF_DTYPE_F8) {
+      const uint8_t *ke = k_exps + (int64_t)tile * kTile, *ve = v_exps + (int64_t)tile * kTile;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int key = 16 * u + n16;
-        load_dwords(a.k[u], base, (key < left ? key : left - 1) * row_bytes + g * 16 * es);
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int key = 16 * (j >> 2) + 4 * g + (j & 3);
-        load_dwords(a.v[j], base, (key < left ? key : left - 1) * row_bytes + v_off + n16 * 4 * es);
-        if (key >= left)
-#pragma unroll
-          for (int i = 0; i < Tile::VD; ++i) a.v[j][i] = 0;
-      }
-      if constexpr (CACHE == WF_DTYPE_F8)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          a.ke[u] = k_exps[tile * kTile + (16 * u + n16 < left ? 16 * u + n16 : left - 1)];
+        if (left >= kTile) {
+          a.ke[u] = ke[16 * u + n16];
+          __builtin_memcpy(&a.ve[u], ve + 16 * u + 4 * g, 4);
+        } else {
+          a.ke[u] = ke[16 * u + n16 < left ? 16 * u + n16 : left - 1];
           a.ve[u] = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int key = 16 * u + 4 * g + i;
-            a.ve[u] |= (uint32_t)v_exps[tile * kTile + (key < left ? key : left - 1)] << (8 * i);
+            a.ve[u] |= (uint32_t)ve[key < left ? key : left - 1] << (8 * i);
           }
         }
+      }
     }
     if constexpr (MASK) {             // the two words that hold the tile's 32 bits
       const int64_t at = (int64_t)tile * kTile - from;
@@ -407,12 +406,11 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, NQ>())) cache_attention
       float top = x[0];
 #pragma unroll
       for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
-      const Pair rp = row_pair(top);
-      top = half_max(fmaxf(rp.a, rp.b));
-      top = top == -INFINITY ? top : top * c;
       // The reference follows the maximum only where that is 2^8 above it: weights of up to 2^8 lose nothing in fp32.
+      top = top == -INFINITY ? top : top * c;
       if (__ballot(top > w.m + 8.0f)) {
-        top = fmaxf(top, w.m);
+        const Pair rp = row_pair(top);
+        top = fmaxf(w.m, half_max(fmaxf(rp.a, rp.b)));
         const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - top);
         w.l *= keep;
 #pragma unroll
@@ -431,10 +429,9 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, NQ>())) cache_attention
       if constexpr (BF) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bf16x2 b = {(__bf16)x[2 * j], (__bf16)x[2 * j + 1]};
-          const bf16x2 r = {(__bf16)(x[2 * j] - (float)b[0]), (__bf16)(x[2 * j + 1] - (float)b[1])};
-          hi[j] = pack(b);
-          lo[j] = pack(r);
+          hi[j] = pack(__builtin_convertvector(f32x2{x[2 * j], x[2 * j + 1]}, bf16x2));
+          const f32x2 rest = {x[2 * j] - __builtin_bit_cast(float, hi[j] << 16), x[2 * j + 1] - __builtin_bit_cast(float, hi[j] & 0xffff0000u)};
+          lo[j] = pack(__builtin_convertvector(rest, bf16x2));
         }
       }
       auto second = [&](const uint32_t (&v)[BF ? 4 : 8], const uint32_t (&v_lo)[BF ? 4 : 8], f32x4 o) -> f32x4 {
@@ -464,16 +461,19 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, NQ>())) cache_attention
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[t].o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
+  constexpr int D = CACHE == WF_DTYPE_F8 ? 2 : 2;      // tiles of a wave in registers: one in use, the others on their way
+  Tile ring[D];
   int tile = t_first;
-  Tile a, b;
-  if (tile < t_end) load(a, tile);
+#pragma unroll
+  for (int i = 0; i < D - 1; ++i)
+    if (tile + i * NW < t_end) load(ring[i], tile + i * NW);
   while (tile < t_end) {
-    if (tile + NW < t_end) load(b, tile + NW);
-    compute(a, tile);
-    if ((tile += NW) >= t_end) break;
-    if (tile + NW < t_end) load(a, tile + NW);
-    compute(b, tile);
-    tile += NW;
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      if (tile + (D - 1) * NW < t_end) load(ring[(i + D - 1) % D], tile + (D - 1) * NW);
+      compute(ring[i], tile);
+      if ((tile += NW) >= t_end) break;
+    }
   }
   const bool whole = p.n_split == 1 || n <= p.split_keys;      // no other workgroup has keys of this sequence
   const int64_t part_at = (((int64_t)s * H + h) * p.chunks + chunk) * 16 * NQ * p.n_split + z;      // of row 0 of the chunk; a row on: n_split
