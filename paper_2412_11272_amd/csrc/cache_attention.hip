@@ -434,15 +434,6 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
           lo[j] = pack(__builtin_convertvector(rest, bf16x2));
         }
       }
-      auto second = [&](const uint32_t (&v)[BF ? 4 : 8], const uint32_t (&v_lo)[BF ? 4 : 8], f32x4 o) -> f32x4 {
-        if constexpr (BF) {
-          return mma(v, hi, mma(v_lo, lo, o));
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) o = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[j]), x[j], o, 0, 0, 0);
-          return o;
-        }
-      };
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if constexpr (BF) {
@@ -555,11 +546,12 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
   }
 }
 
-// The parts of the rows whose keys several workgroups shared: 16 lanes a row.
+// The parts of the rows whose keys several workgroups shared: a wave a row.  Lane z has the maximum and sum of part z; the values are added by
+// 16 lanes, four parts at a time.
 template <typename T>
 __global__ void __launch_bounds__(256) cache_attention_join_kernel(AttendArgs p, int rows_pad) {
-  const int64_t unit = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int d = (threadIdx.x & 15) * 4, H = p.c.n_heads;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, d = (lane & 15) * 4, H = p.c.n_heads;
   const int64_t sh = unit / rows_pad;
   if (sh >= (int64_t)p.n_seqs * H) return;
   const int row = (int)(unit % rows_pad), s = (int)(sh / H), h = (int)(sh % H);
@@ -569,18 +561,34 @@ __global__ void __launch_bounds__(256) cache_attention_join_kernel(AttendArgs p,
   const int n = sequence_keys(p, s, &row0);
   if (n <= p.split_keys) return;
   const int parts = (n + p.split_keys - 1) / p.split_keys;
-  const float *ml = p.part_ml + 2 * unit * p.n_split, *part = p.part + unit * p.n_split * 64 + d;
-  float m = -INFINITY;
-  for (int z = 0; z < parts; ++z) m = fmaxf(m, ml[2 * z]);
-  const float base = m == -INFINITY ? 0.0f : m;
+  static_assert(kMaxSplits <= 64, "a lane per part");
+  const f32x2 ml = lane < parts ? *(const f32x2 *)(p.part_ml + 2 * (unit * p.n_split + lane)) : f32x2{-INFINITY, 0.0f};
+  const float m_one = ml[0], l_one = ml[1];
+  const float m = wave_max(m_one), base = m == -INFINITY ? 0.0f : m;
+  const float f_one = l_one == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m_one - base);      // no sum: saw nothing
+  const float l = wave_sum(l_one * f_one);
+  const float *part = p.part + unit * p.n_split * 64 + d;
   f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-  float l = 0.0f;
-  for (int z = 0; z < parts; ++z) {
-    if (ml[2 * z + 1] == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml[2 * z] - base);
-    o += *(const f32x4 *)(part + z * 64) * f;
-    l += ml[2 * z + 1] * f;
+  for (int z0 = 0; z0 < parts; z0 += 16) {
+    f32x4 v[4];
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int z = z0 + 4 * i + (lane >> 4);
+      f[i] = __shfl(f_one, z & 63);
+      v[i] = z < parts ? *(const f32x4 *)(part + (int64_t)z * 64) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (z0 + 4 * i + (lane >> 4) < parts && f[i] != 0.0f) o += v[i] * f[i];
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float x = o[i];
+    const Pair rp = row_pair(x);
+    o[i] = half_sum(rp.a + rp.b);
+  }
+  if (lane >= 16) return;
   const float inv = l != 0.0f ? 1.0f / l : 0.0f;
   o *= inv;
   T *dst = (T *)p.out + (int64_t)(q_first + row / p.group) * p.ldo + (h * p.group + row % p.group) * 64 + d;
@@ -597,9 +605,9 @@ Plan plan_of(const wf_cache &c, const wf_cache_query &a) {
   const int64_t rows = (int64_t)std::min(a.max_q, std::max(a.n_q_rows, 1)) * (a.n_heads / c.n_heads);
   p.nq = rows <= 16 ? 1 : rows <= 32 || a.dtype == WF_DTYPE_F32 ? 2 : 4;      // 64 rows of fp32 operands outgrow the registers
   p.chunks = (int)((rows + 16 * p.nq - 1) / (16 * p.nq));
-  const int64_t groups = (int64_t)a.n_seqs * c.n_heads * p.chunks, want = 1024;
+  const int64_t groups = (int64_t)a.n_seqs * c.n_heads * p.chunks, want = p.nq > 1 ? 2048 : 1024;
   int64_t n = groups >= want ? 1 : (want + groups - 1) / groups;
-  const int64_t most = std::max<int64_t>(1, a.max_len / 1024);
+  const int64_t most = std::max<int64_t>(1, a.max_len / 768);
   n = std::min<int64_t>(std::min(n, most), kMaxSplits);
   p.split_keys = (int)std::min<int64_t>(host::round_up(std::max<int64_t>((a.max_len + n - 1) / n, kTile), kTile), INT32_MAX / kTile * kTile);
   p.n_split = (int)std::max<int64_t>(1, ((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
@@ -695,7 +703,7 @@ int wf_op_cache_attention(const wf_cache *cache, const wf_cache_query *query, vo
   }
   if (parts) {
     const int rows_pad = plan.chunks * 16 * plan.nq;
-    const dim3 join((uint32_t)(((int64_t)a.n_seqs * cache->n_heads * rows_pad + 15) / 16));
+    const dim3 join((uint32_t)(((int64_t)a.n_seqs * cache->n_heads * rows_pad + 3) / 4));
     if (a.dtype == WF_DTYPE_BF16) cache_attention_join_kernel<__bf16><<<join, 256, 0, s>>>(p, rows_pad);
     else cache_attention_join_kernel<float><<<join, 256, 0, s>>>(p, rows_pad);
   }
