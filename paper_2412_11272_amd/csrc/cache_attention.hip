@@ -23,6 +23,7 @@
 #include "host_runtime.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace wf {
 
@@ -128,7 +129,7 @@ __device__ __forceinline__ f32x4 mma(const uint32_t (&a)[4], const uint32_t (&b)
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
 }
 
-// A wave's running state for 16 query rows: lane (n, g) has row n's maximum (in powers of two), its share of the sum, and values 16 g + 4 i + t.
+// A wave's running state for 16 query rows: lane (n, g) has row n's reference (in powers of two), its share of the sum, and values 16 g + 4 i + t.
 struct State {
   float m, l;
   f32x4 o[4];
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
     chunk = id / 8 % p.chunks;
     id = id / (8 * p.chunks) * 8 + id % 8;
   }
-  const int h = id % H; id /= H;
+  const int h = (id % H + id / H) % H; id /= H;
   const int s = id % p.n_seqs, z = id / p.n_seqs;
   if (z >= p.n_split) return;
 
@@ -303,7 +304,9 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
   State st[NQ];
   const float c = fabsf(p.scale) * 1.4426950408889634f;      // exp(s scale) = exp2(s c)
 
-  auto compute = [&](const Tile &a, int tile) {
+  // FREE: every row sees every key of the tile.
+  auto compute = [&](const Tile &a, int tile, auto free) {
+    constexpr bool FREE = decltype(free)::value;
     // ---- values: pairs of keys next to each other
     uint32_t vt[4][BF ? 4 : 8];
     if constexpr (BF) {
@@ -362,21 +365,25 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
         for (int i = 0; i < QD; ++i) kt[u][i] = a.k[u][i];
       }
     }
-    const bool whole_tile = n - tile * kTile >= kTile && (!MASK || (int64_t)(tile + 1) * kTile <= from);      // every row sees every key
+    // Two query tiles side by side: one's matrix instructions beside the other's exponentials
+    constexpr int GT = NQ < 2 ? NQ : 2;
 #pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      if (t > 0 && t >= n_tiles_q) break;
-      State &w = st[t];
+    for (int t0 = 0; t0 < NQ; t0 += GT) {
+    if (t0 > 0 && t0 >= n_tiles_q) break;
+    float x[GT][8];
+    bool rise = false;
+#pragma unroll
+    for (int k = 0; k < GT; ++k) {
+      const int t = t0 + k;
       uint32_t qa[QD];
 #pragma unroll
       for (int i = 0; i < QD; ++i) qa[i] = q_one[i];
       if constexpr (NQ > 1)
 #pragma unroll
         for (int i = 0; i < QD / 4; ++i) {
-          const u32x4 x = s_q[t][i][lane];
-          qa[4 * i] = x[0]; qa[4 * i + 1] = x[1]; qa[4 * i + 2] = x[2]; qa[4 * i + 3] = x[3];
+          const u32x4 y = s_q[t][i][lane];
+          qa[4 * i] = y[0]; qa[4 * i + 1] = y[1]; qa[4 * i + 2] = y[2]; qa[4 * i + 3] = y[3];
         }
-      float x[8];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         f32x4 d{0.0f, 0.0f, 0.0f, 0.0f};
@@ -393,56 +400,61 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
             d = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kt[u][i]), __builtin_bit_cast(float, qa[i]), d, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * u + i] = d[i];
+        for (int i = 0; i < 4; ++i) x[k][4 * u + i] = d[i];
       }
-      uint32_t seen = ~0u;
-      if (!whole_tile) {
-        seen = seen_keys(a, tile, t);
-        const uint32_t mine = seen >> (4 * g);
+      if constexpr (!FREE) {
+        const uint32_t mine = seen_keys(a, tile, t) >> (4 * g);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (!(mine >> (16 * (j >> 2) + (j & 3)) & 1)) x[j] = -INFINITY;
+          if (!(mine >> (16 * (j >> 2) + (j & 3)) & 1)) x[k][j] = -INFINITY;
       }
-      float top = x[0];
+      float top = x[k][0];
 #pragma unroll
-      for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
-      // The reference follows the maximum only where that is 2^8 above it: weights of up to 2^8 lose nothing in fp32.
-      top = top == -INFINITY ? top : top * c;
-      if (__ballot(top > w.m + 8.0f)) {
+      for (int j = 1; j < 8; ++j) top = fmaxf(top, x[k][j]);
+      rise |= (top > -INFINITY) & (top * c > st[t].m + 8.0f);
+    }
+    // A row's reference follows its maximum only where that is 2^8 above it: weights of up to 2^8 lose nothing in fp32.
+    if (__ballot(rise)) {
+#pragma unroll
+      for (int k = 0; k < GT; ++k) {
+        State &w = st[t0 + k];
+        float top = x[k][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[k][j]);
         const Pair rp = row_pair(top);
-        top = fmaxf(w.m, half_max(fmaxf(rp.a, rp.b)));
+        top = half_max(fmaxf(rp.a, rp.b));
+        top = top == -INFINITY ? w.m : fmaxf(w.m, top * c);
         const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - top);
         w.l *= keep;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w.o[i] *= keep;
         w.m = top;
       }
-      const float base = w.m == -INFINITY ? 0.0f : w.m;
-      float sum = 0.0f;
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], c, -base));
-        sum += x[j];
-      }
-      w.l += sum;
-      uint32_t hi[4], lo[4];
+    for (int k = 0; k < GT; ++k) {
+      State &w = st[t0 + k];
+      const float base = w.m == -INFINITY ? 0.0f : w.m;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[k][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][j], c, -base));
+      w.l += ((x[k][0] + x[k][1]) + (x[k][2] + x[k][3])) + ((x[k][4] + x[k][5]) + (x[k][6] + x[k][7]));
       if constexpr (BF) {
+        uint32_t hi[4], lo[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          hi[j] = pack(__builtin_convertvector(f32x2{x[2 * j], x[2 * j + 1]}, bf16x2));
-          const f32x2 rest = {x[2 * j] - __builtin_bit_cast(float, hi[j] << 16), x[2 * j + 1] - __builtin_bit_cast(float, hi[j] & 0xffff0000u)};
+          hi[j] = pack(__builtin_convertvector(f32x2{x[k][2 * j], x[k][2 * j + 1]}, bf16x2));
+          const f32x2 rest = {x[k][2 * j] - __builtin_bit_cast(float, hi[j] << 16), x[k][2 * j + 1] - __builtin_bit_cast(float, hi[j] & 0xffff0000u)};
           lo[j] = pack(__builtin_convertvector(rest, bf16x2));
         }
-      }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (BF) {
-          w.o[i] = mma(vt[i], hi, mma(vt[i], lo, w.o[i]));
-        } else {
+        for (int i = 0; i < 4; ++i) w.o[i] = mma(vt[i], hi, mma(vt[i], lo, w.o[i]));
+      } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) w.o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vt[i][j]), x[j], w.o[i], 0, 0, 0);
-        }
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w.o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vt[i][j]), x[k][j], w.o[i], 0, 0, 0);
       }
+    }
     }
   };
 #pragma unroll
@@ -452,19 +464,31 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[t].o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  constexpr int D = CACHE == WF_DTYPE_F8 ? 2 : 2;      // tiles of a wave in registers: one in use, the others on their way
+  constexpr int D = 2;      // tiles of a wave in registers: one in use, one on its way
   Tile ring[D];
   int tile = t_first;
 #pragma unroll
   for (int i = 0; i < D - 1; ++i)
     if (tile + i * NW < t_end) load(ring[i], tile + i * NW);
-  while (tile < t_end) {
+  const int t_free = MASK ? (int)((from < n ? from > 0 ? from : 0 : n) / kTile) : n / kTile;      // tiles before it are free
+  while (tile < t_end && tile < t_free) {
 #pragma unroll
     for (int i = 0; i < D; ++i) {
       if (tile + (D - 1) * NW < t_end) load(ring[(i + D - 1) % D], tile + (D - 1) * NW);
-      compute(ring[i], tile);
-      if ((tile += NW) >= t_end) break;
+      compute(ring[i], tile, std::true_type{});
+      tile += NW;
+      if (tile >= t_end || tile >= t_free) {
+        if (i + 1 < D) ring[0] = ring[i + 1];
+        break;
+      }
     }
+  }
+  while (tile < t_end) {
+    static_assert(D == 2, "one tile ahead");
+    if (tile + NW < t_end) load(ring[1], tile + NW);
+    compute(ring[0], tile, std::false_type{});
+    ring[0] = ring[1];
+    tile += NW;
   }
   const bool whole = p.n_split == 1 || n <= p.split_keys;      // no other workgroup has keys of this sequence
   const int64_t part_at = (((int64_t)s * H + h) * p.chunks + chunk) * 16 * NQ * p.n_split + z;      // of row 0 of the chunk; a row on: n_split
