@@ -621,7 +621,7 @@ __global__ void __launch_bounds__(256) cache_attention_join_kernel(AttendArgs p,
 }
 
 struct Plan {
-  int nq, chunks, n_split, split_keys;
+  int nq, nw, chunks, n_split, split_keys;
 };
 
 Plan plan_of(const wf_cache &c, const wf_cache_query &a) {
@@ -635,25 +635,23 @@ Plan plan_of(const wf_cache &c, const wf_cache_query &a) {
   n = std::min<int64_t>(std::min(n, most), kMaxSplits);
   p.split_keys = (int)std::min<int64_t>(host::round_up(std::max<int64_t>((a.max_len + n - 1) / n, kTile), kTile), INT32_MAX / kTile * kTile);
   p.n_split = (int)std::max<int64_t>(1, ((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
+  p.nw = p.nq > 1 || groups < 1024 || a.max_len > 256 ? 4 : a.max_len > 64 ? 2 : 1;
   return p;
 }
 
-template <typename T, int CACHE, int NQ, bool MASK>
+template <typename T, int CACHE, int NQ, int NW>
 void launch_attend(const AttendArgs &p, dim3 grid, hipStream_t s) {
-  cache_attention_kernel<T, CACHE, NQ, 4, MASK><<<grid, 256, 0, s>>>(p);
+  if (p.mask) cache_attention_kernel<T, CACHE, NQ, NW, true><<<grid, 64 * NW, 0, s>>>(p);
+  else cache_attention_kernel<T, CACHE, NQ, NW, false><<<grid, 64 * NW, 0, s>>>(p);
 }
 
 template <typename T, int CACHE>
-void launch_attend(const AttendArgs &p, int nq, dim3 grid, hipStream_t s) {
-  if (p.mask) {
-    if (nq == 1) launch_attend<T, CACHE, 1, true>(p, grid, s);
-    else if (nq == 2) launch_attend<T, CACHE, 2, true>(p, grid, s);
-    else if constexpr (sizeof(T) == 2) launch_attend<T, CACHE, 4, true>(p, grid, s);
-  } else {
-    if (nq == 1) launch_attend<T, CACHE, 1, false>(p, grid, s);
-    else if (nq == 2) launch_attend<T, CACHE, 2, false>(p, grid, s);
-    else if constexpr (sizeof(T) == 2) launch_attend<T, CACHE, 4, false>(p, grid, s);
-  }
+void launch_attend(const AttendArgs &p, const Plan &plan, dim3 grid, hipStream_t s) {
+  if (plan.nq == 1 && plan.nw == 1) launch_attend<T, CACHE, 1, 1>(p, grid, s);
+  else if (plan.nq == 1 && plan.nw == 2) launch_attend<T, CACHE, 1, 2>(p, grid, s);
+  else if (plan.nq == 1) launch_attend<T, CACHE, 1, 4>(p, grid, s);
+  else if (plan.nq == 2) launch_attend<T, CACHE, 2, 4>(p, grid, s);
+  else if constexpr (sizeof(T) == 2) launch_attend<T, CACHE, 4, 4>(p, grid, s);
 }
 
 }  // namespace
@@ -719,11 +717,11 @@ int wf_op_cache_attention(const wf_cache *cache, const wf_cache_query *query, vo
   const dim3 grid((uint32_t)groups);
   const hipStream_t s = (hipStream_t)hip_stream;
   if (a.dtype == WF_DTYPE_BF16) {
-    if (cache->dtype == WF_DTYPE_F8) launch_attend<__bf16, WF_DTYPE_F8>(p, plan.nq, grid, s);
-    else launch_attend<__bf16, WF_DTYPE_BF16>(p, plan.nq, grid, s);
+    if (cache->dtype == WF_DTYPE_F8) launch_attend<__bf16, WF_DTYPE_F8>(p, plan, grid, s);
+    else launch_attend<__bf16, WF_DTYPE_BF16>(p, plan, grid, s);
   } else {
-    if (cache->dtype == WF_DTYPE_F8) launch_attend<float, WF_DTYPE_F8>(p, plan.nq, grid, s);
-    else launch_attend<float, WF_DTYPE_F32>(p, plan.nq, grid, s);
+    if (cache->dtype == WF_DTYPE_F8) launch_attend<float, WF_DTYPE_F8>(p, plan, grid, s);
+    else launch_attend<float, WF_DTYPE_F32>(p, plan, grid, s);
   }
   if (parts) {
     const int rows_pad = plan.chunks * 16 * plan.nq;
