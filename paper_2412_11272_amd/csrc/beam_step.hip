@@ -19,7 +19,7 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 __device__ __forceinline__ float value_of(uint32_t order) {
   return __builtin_bit_cast(float, order & 0x80000000u ? order & 0x7fffffffu : ~order);
 }
-__device__ __forceinline__ bool is_finite(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7f800000u) != 0x7f800000u; }
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
 
 // Between a wave's writes to the LDS and its other lanes' reads: the LDS works in order, so only the compiler has to keep it.
 __device__ __forceinline__ void wave_sync() {
@@ -27,7 +27,7 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Maxima over a wave by the same lane moves as device_utils.h's, on two registers.
+// Maxima and sums over a wave by the same lane moves as device_utils.h's, on two registers.
 template <typename U, int N>
 __device__ __forceinline__ U row_rotate64(U v) {
   const u32x2 u = __builtin_bit_cast(u32x2, v);
@@ -35,34 +35,35 @@ __device__ __forceinline__ U row_rotate64(U v) {
   const u32x2 r = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)lo, 0x120 + N, 0xF, 0xF, true), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)hi, 0x120 + N, 0xF, 0xF, true)};
   return __builtin_bit_cast(U, r);
 }
-template <typename U>
-__device__ __forceinline__ U max64(U a, U b) { return a > b ? a : b; }
-template <typename U>
-__device__ __forceinline__ U wave_max64(U v) {
-  v = max64(v, row_rotate64<U, 8>(v));
-  v = max64(v, row_rotate64<U, 4>(v));
-  v = max64(v, row_rotate64<U, 2>(v));
-  v = max64(v, row_rotate64<U, 1>(v));
+template <typename U, typename F>
+__device__ __forceinline__ U wave_reduce64(U v, F f) {
+  v = f(v, row_rotate64<U, 8>(v));
+  v = f(v, row_rotate64<U, 4>(v));
+  v = f(v, row_rotate64<U, 2>(v));
+  v = f(v, row_rotate64<U, 1>(v));
   u32x2 u = __builtin_bit_cast(u32x2, v);
   uint32_t lo = u[0], hi = u[1];
   const auto l16 = __builtin_amdgcn_permlane16_swap(lo, lo, false, false), h16 = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
   const u32x2 a = {(uint32_t)l16[0], (uint32_t)h16[0]}, b = {(uint32_t)l16[1], (uint32_t)h16[1]};
-  u = __builtin_bit_cast(u32x2, max64(__builtin_bit_cast(U, a), __builtin_bit_cast(U, b)));
+  u = __builtin_bit_cast(u32x2, f(__builtin_bit_cast(U, a), __builtin_bit_cast(U, b)));
   lo = u[0]; hi = u[1];
   const auto l32 = __builtin_amdgcn_permlane32_swap(lo, lo, false, false), h32 = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
   const u32x2 c = {(uint32_t)l32[0], (uint32_t)h32[0]}, d = {(uint32_t)l32[1], (uint32_t)h32[1]};
-  return max64(__builtin_bit_cast(U, c), __builtin_bit_cast(U, d));
+  return f(__builtin_bit_cast(U, c), __builtin_bit_cast(U, d));
 }
-__device__ __forceinline__ double wave_sum_f64(double v) {
-  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-  return v;
-}
+template <typename U>
+__device__ __forceinline__ U max64(U a, U b) { return a > b ? a : b; }
+template <typename U>
+__device__ __forceinline__ U wave_max64(U v) { return wave_reduce64(v, max64<U>); }
+__device__ __forceinline__ double wave_sum_f64(double v) { return wave_reduce64(v, [](double a, double b) { return a + b; }); }
 
-// Part of a beam's row: the maximum and sum of its exponentials, and its best candidates as keys (0: no more).
+// Part of a beam's row: the sum of 2^(x kLog2e - base) over its values x (no finite one: base = -infinity), and its best candidates as keys (0: no
+// more).  kLog2e is the fp32 value and the sum's logarithm is divided by that very number, so that its rounding, 1.3e-8, costs the entropy times that
+// much, and not the logits.
 struct PartSum {
-  double sum;
-  float top, unused;
+  double sum, base;
 };
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct SelectArgs {
   const void *logits;
@@ -107,10 +108,11 @@ __global__ void __launch_bounds__(256) beam_parts_kernel(SelectArgs p) {
   constexpr int N = Values<T>::N, CH = 32 / N;
   __shared__ uint64_t s_keys[4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  const int row = (int)(id / p.parts), part = (int)(id % p.parts);
+  const int row = blockIdx.x, part = blockIdx.y * 4 + wave;
+  if (part >= p.parts) return;
   const int s = row / p.width, b = row % p.width;
-  if (s >= p.B || b >= clamped(p.n_in, s, p.width) || (p.done_in && p.done_in[row])) return;
+  if (b >= clamped(p.n_in, s, p.width) || (p.done_in && p.done_in[row])) return;
+  const int64_t id = (int64_t)row * p.parts + part;
   const T *x = (const T *)p.logits + (int64_t)row * p.ld + (int64_t)part * kPart;
   const int left = p.n_vocab - part * kPart;
   float v[32];
@@ -141,20 +143,27 @@ __global__ void __launch_bounds__(256) beam_parts_kernel(SelectArgs p) {
   uint64_t *keys = p.keys + id * W;
   if (top == -INFINITY) {
     if (lane < W) keys[lane] = 0;
-    if (lane == 0) p.sums[id] = PartSum{0.0, -INFINITY, 0.0f};
+    if (lane == 0) p.sums[id] = PartSum{0.0, -(double)INFINITY};
     return;
   }
   // The sum: eight values in 32 bits, the rest in 64
+  const bool huge = fabsf(top) > 0x1p100f;      // top * kLog2e may overflow
+  const float base = top * kLog2e;
   double sum = 0.0;
+  if (!huge) {
 #pragma unroll
-  for (int i = 0; i < 32; i += 8) {
-    float f = 0.0f;
+    for (int i = 0; i < 32; i += 8) {
+      float f = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f += __builtin_amdgcn_exp2f((v[i + e] - top) * 1.4426950408889634f);
-    sum += f;
+      for (int e = 0; e < 8; ++e) f += __builtin_amdgcn_exp2f(__builtin_fmaf(v[i + e], kLog2e, -base));
+      sum += f;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sum += __builtin_amdgcn_exp2f((v[i] - top) * kLog2e);
   }
   sum = wave_sum_f64(sum);
-  if (lane == 0) p.sums[id] = PartSum{sum, top, 0.0f};
+  if (lane == 0) p.sums[id] = PartSum{sum, huge ? (double)top * kLog2e : (double)base};
 
   const uint32_t order = mine == -INFINITY ? 0 : order_of(mine);
   uint32_t bound = 0;
@@ -199,37 +208,45 @@ __global__ void __launch_bounds__(256) beam_parts_kernel(SelectArgs p) {
   }
 }
 
-// One workgroup per stream.  A wave joins a beam's parts: the log of its sum, and the best of its parts' candidates.  Then the first wave merges the
-// beams' sorted candidates, lane b holding the first of beam b that is not taken yet.
+// One workgroup per stream.  One wave joins the sums of a beam's parts, another takes the best of the parts' candidates.  Then the first wave merges
+// the beams' sorted candidates, lane b holding the first of beam b that is not taken yet.
 constexpr int kHeld = 4;      // keys of a beam that a lane keeps in registers
-__global__ void __launch_bounds__(512) beam_merge_kernel(SelectArgs p) {
+__global__ void __launch_bounds__(1024) beam_merge_kernel(SelectArgs p) {
   __shared__ uint64_t s_key[kMaxBeams][kMaxBeams];
   __shared__ double s_log[kMaxBeams];
   __shared__ int32_t s_token[kMaxBeams], s_parent[kMaxBeams], s_slot[kMaxBeams];
   __shared__ float s_score[kMaxBeams];
   const int s = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, W = p.width;
   const int n_in = clamped(p.n_in, s, W), n_out = clamped(p.n_out, s, W);
-  for (int b = wave; b < n_in; b += waves) {
+  const float start = lane < n_in ? p.score_in[(int64_t)s * W + lane] : -INFINITY;      // read before any output is written: it may be the same memory
+  const bool live = lane < n_in && is_finite(start);
+  const bool was_done = live && p.done_in && p.done_in[(int64_t)s * W + lane];
+  for (int job = wave; job < 2 * n_in; job += waves) {
+    const int b = job >> 1;
     const int64_t row = (int64_t)s * W + b;
-    if (p.done_in && p.done_in[row]) {
-      if (lane < W) s_key[b][lane] = lane == 0 ? key_of(0.0f, p.eos) : 0;
-      if (lane == 0) s_log[b] = 0.0;
+    const bool done = p.done_in && p.done_in[row];
+    if (job & 1) {
+      const PartSum *sums = p.sums + row * p.parts;
+      double base = -INFINITY, sum = 0.0;
+      if (!done) {
+        for (int i = lane; i < p.parts; i += 64) base = max64(base, sums[i].base);
+        base = wave_max64(base);
+        for (int i = lane; i < p.parts; i += 64)
+          if (sums[i].base != -INFINITY) sum += sums[i].sum * exp2(sums[i].base - base);
+        sum = wave_sum_f64(sum);
+      }
+      if (lane == 0) s_log[b] = done ? 0.0 : (base + log2(sum)) / (double)kLog2e;
       continue;
     }
-    const PartSum *sums = p.sums + row * p.parts;
+    if (done) {
+      if (lane < W) s_key[b][lane] = lane == 0 ? key_of(0.0f, p.eos) : 0;
+      continue;
+    }
     const uint64_t *keys = p.keys + row * p.parts * W;
     const int n = p.parts * W;
     uint64_t held[kHeld];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) held[i] = lane + 64 * i < n ? keys[lane + 64 * i] : 0;
-    float top = -INFINITY;
-    for (int i = lane; i < p.parts; i += 64) top = fmaxf(top, sums[i].top);
-    top = wave_max(top);
-    double sum = 0.0;
-    for (int i = lane; i < p.parts; i += 64)
-      if (sums[i].top != -INFINITY) sum += sums[i].sum * exp((double)sums[i].top - (double)top);
-    sum = wave_sum_f64(sum);
-    if (lane == 0) s_log[b] = (double)top + log(sum);
     uint64_t last = ~0ull;
     for (int k = 0; k < W; ++k) {
       uint64_t best = 0;
@@ -246,9 +263,6 @@ __global__ void __launch_bounds__(512) beam_merge_kernel(SelectArgs p) {
   }
   __syncthreads();
   if (wave > 0) return;
-  const float start = lane < n_in ? p.score_in[(int64_t)s * W + lane] : -INFINITY;
-  const bool live = lane < n_in && is_finite(start);
-  const bool was_done = live && p.done_in && p.done_in[(int64_t)s * W + lane];
   const double log_sum = live ? s_log[lane] : 0.0;
   int at = 0;
   uint64_t key = live ? s_key[lane][0] : 0;
@@ -271,9 +285,9 @@ __global__ void __launch_bounds__(512) beam_merge_kernel(SelectArgs p) {
     }
   }
   wave_sync();
-  if (lane == 0) {
-    for (int j = 0; j < W; ++j) s_slot[j] = !p.keep_slots && j < n ? j : -1;
-    if (p.keep_slots) {
+  if (p.keep_slots) {
+    if (lane == 0) {
+      for (int j = 0; j < W; ++j) s_slot[j] = -1;
       uint32_t placed = 0;
       for (int j = 0; j < n; ++j)
         if (s_parent[j] < n_out && s_slot[s_parent[j]] < 0) { s_slot[s_parent[j]] = j; placed |= 1u << j; }
@@ -284,11 +298,11 @@ __global__ void __launch_bounds__(512) beam_merge_kernel(SelectArgs p) {
         s_slot[free] = j;
       }
     }
+    wave_sync();
   }
-  wave_sync();
   if (lane < W) {
     const int64_t o = (int64_t)s * W + lane;
-    const int j = s_slot[lane];
+    const int j = p.keep_slots ? s_slot[lane] : lane < n ? lane : -1;
     p.token_out[o] = j < 0 ? -1 : s_token[j] & 0x7fffffff;
     p.parent_out[o] = j < 0 ? -1 : s_parent[j];
     p.score_out[o] = j < 0 ? -INFINITY : s_score[j];
@@ -368,7 +382,7 @@ int check_step(const wf_beam_step *a) {
   if (a->width < 1 || a->width > kMaxBeams) return fail(WF_E_INVALID_ARG, "width = %d (supported: 1 .. %d)", a->width, kMaxBeams);
   if (a->n_vocab < 1) return fail(WF_E_INVALID_ARG, "n_vocab = %d", a->n_vocab);
   if ((int64_t)a->B * a->width >= 1 << 22) return fail(WF_E_CAPACITY, "B * width = %lld beams (supported: below 2^22)", (long long)a->B * a->width);
-  if ((int64_t)a->B * a->width * parts_of(a->n_vocab) >= (int64_t)1 << 32)
+  if (a->n_vocab > 1 << 29 || (int64_t)a->B * a->width * parts_of(a->n_vocab) >= (int64_t)1 << 32)
     return fail(WF_E_CAPACITY, "%d streams of %d beams over %d tokens: too many parts", a->B, a->width, a->n_vocab);
   return WF_OK;
 }
@@ -398,10 +412,10 @@ int wf_op_beam_select(const wf_beam_step *a, void *hip_stream) {
   const SelectArgs p{a->logits_dev, a->ld, a->n_in_dev, a->n_out_dev, a->score_in_dev, a->done_in_dev, a->token_out_dev, a->parent_out_dev, a->score_out_dev,
                      a->done_out_dev, sums, (uint64_t *)(sums + waves), a->B, a->width, a->n_vocab, a->done_in_dev ? a->eos : -1, a->keep_slots, parts};
   const hipStream_t s = (hipStream_t)hip_stream;
-  const dim3 grid((uint32_t)((waves + 3) / 4));
+  const dim3 grid(a->B * a->width, (parts + 3) / 4);
   if (a->dtype == WF_DTYPE_BF16) beam_parts_kernel<__bf16><<<grid, 256, 0, s>>>(p);
   else beam_parts_kernel<float><<<grid, 256, 0, s>>>(p);
-  beam_merge_kernel<<<a->B, 64 * std::min(a->width, 8), 0, s>>>(p);
+  beam_merge_kernel<<<a->B, 64 * std::min(2 * a->width, 16), 0, s>>>(p);
   const hipError_t err = hipGetLastError();
   return err == hipSuccess ? WF_OK : fail(WF_E_HIP, "beam_select launch: %s", hipGetErrorString(err));
 }
