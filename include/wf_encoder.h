@@ -508,7 +508,7 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *                     ld elements (>= 64 * n_heads; both pointers and ld * element size multiples of 16 bytes).  F8: each head's key and
  *                     value vector gets the smallest power of two 2^e >= 2^-127 with max|x| <= 448 * 2^e and is rounded to nearest even;
  *                     a value that is not finite is stored as NaN and does not count in the maximum.  Others: rounded to nearest even.
- *                     Tokens at or behind cu_dev[B] and rows outside the cache are left out; other rows stay as they were.
+ *                     Tokens at or behind cu_dev[B] and rows outside the cache are left out; other rows stay as they were.  n_tokens < 2^26.
  * wf_op_cache_read    the same rows back: out_dev [n_tokens, 2 * 64 * n_heads] (keys of all heads, then values) of dtype f32 or bf16, contiguous.
  *                     Tokens behind the last sequence keep what out_dev holds; those whose row lies outside the cache read as zero.
  * wf_op_cache_attention   out[r, h, :] = sum_k w_k v_k, w = softmax over the visible keys k of scale * q[r, h, :] . k.  Row r of q, cu_q_dev[s] <= r
@@ -532,12 +532,14 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *                     candidate hold -1, -1, -infinity, 0; done_out = the parent was done or the token is eos.  keep_slots != 0: the
  *                     same candidates, ordered so that of each parent's children the best stays in the parent's slot (where that is one
  *                     of the n_out[s]) and the others fill the free slots from the lowest, best first: wf_op_beam_reorder then moves only slots
- *                     whose beam died.  score_out may be score_in, done_out may be done_in.  1 <= width <= 32.  workspace_dev: at least
- *                     wf_beam_select_workspace(..) bytes, aligned to 16, of any content.
+ *                     whose beam died.  score_out may be score_in, done_out may be done_in.  1 <= width <= 32, n_vocab <= 2^28.  workspace_dev: at
+ *                     least wf_beam_select_workspace(..) bytes, aligned to 16, of any content.
  * wf_op_beam_reorder  slot (s, j) of every layer takes over slot (s, parent[s, j]): a slot is n_pos positions of pos_bytes bytes, slot (s, j) of layer
  *                     l starts at byte (l * B * width + s * width + j) * n_pos * pos_bytes of src_dev and dst_dev, and the first
  *                     len_dev[s] positions (DEVICE int32 [B]; NULL: n_pos; clamped to 0 .. n_pos) are moved.  dst_dev == src_dev works in
  *                     place, for any parents; otherwise the two must not overlap.  A parent outside 0 .. width - 1 leaves dst's slot as it was.
+ *                     Both addresses and pos_bytes multiples of 16 (or of 4) move faster than bytes.  WF_E_CAPACITY beyond 2^32 threads of one
+ *                     such piece each.
  */
 #define WF_DTYPE_F8 2
 

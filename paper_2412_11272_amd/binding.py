@@ -774,6 +774,12 @@ def _empty(shape, dtype, like, stream):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _like(t, dtype, stream):
+    """The same of a contiguous tensor's shape."""
+    import torch
+    return torch.empty_like(t, dtype=dtype) if stream is None else _empty(t.shape, dtype, t, stream)
+
+
 def _fill_workspace(a, need: int, workspace, like, here: int, stream):
     """Sets the call's workspace, its own where the caller gives none; the result has to live until the call is made."""
     import torch
@@ -894,10 +900,8 @@ def op_beam_select(logits, scores, n_in=None, n_out=None, done=None, eos: int = 
     for t in (scores, done):
         if t is not None and (t.shape != (B, W) or t.get_device() != here or not t.is_contiguous()):
             raise ValueError(f"scores, done: {tuple(t.shape)} on {t.device}, need a contiguous [{B}, {W}] beside the logits")
-    token, parent = _empty((B, W), torch.int32, scores, stream), _empty((B, W), torch.int32, scores, stream)
-    score, done_out = _empty((B, W), torch.float32, scores, stream), None
-    if done is not None:
-        done_out = _empty((B, W), done.dtype, done, stream)
+    token, parent, score = _like(scores, torch.int32, stream), _like(scores, torch.int32, stream), _like(scores, torch.float32, stream)
+    done_out = None if done is None else _like(done, done.dtype, stream)
     a = WfBeamStep(logits.data_ptr(), ld, _index(n_in, B, here, "n_in"), _index(n_out, B, here, "n_out"), scores.data_ptr(),
                    done.data_ptr() if done is not None else None, token.data_ptr(), parent.data_ptr(), score.data_ptr(),
                    done_out.data_ptr() if done is not None else None, None, 0, _torch_dtype_code(logits.dtype), B, W, V, eos, 1 if keep_slots else 0)

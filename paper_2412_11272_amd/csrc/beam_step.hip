@@ -382,7 +382,7 @@ int check_step(const wf_beam_step *a) {
   if (a->width < 1 || a->width > kMaxBeams) return fail(WF_E_INVALID_ARG, "width = %d (supported: 1 .. %d)", a->width, kMaxBeams);
   if (a->n_vocab < 1) return fail(WF_E_INVALID_ARG, "n_vocab = %d", a->n_vocab);
   if ((int64_t)a->B * a->width >= 1 << 22) return fail(WF_E_CAPACITY, "B * width = %lld beams (supported: below 2^22)", (long long)a->B * a->width);
-  if (a->n_vocab > 1 << 29 || (int64_t)a->B * a->width * parts_of(a->n_vocab) >= (int64_t)1 << 32)
+  if (a->n_vocab > 1 << 28 || (int64_t)a->B * a->width * parts_of(a->n_vocab) >= (int64_t)1 << 32)
     return fail(WF_E_CAPACITY, "%d streams of %d beams over %d tokens: too many parts", a->B, a->width, a->n_vocab);
   return WF_OK;
 }
@@ -433,8 +433,9 @@ int wf_op_beam_reorder(void *dst_dev, const void *src_dev, const int32_t *parent
   const uintptr_t d = (uintptr_t)dst_dev, f = (uintptr_t)src_dev;
   if (d != f && d < f + (uintptr_t)all && f < d + (uintptr_t)all) return fail(WF_E_INVALID_ARG, "dst_dev and src_dev overlap");
   const int vec = (d | f | (uintptr_t)slot | (uintptr_t)pos_bytes) % 16 == 0 ? 16 : (d | f | (uintptr_t)slot | (uintptr_t)pos_bytes) % 4 == 0 ? 4 : 1;
-  ReorderArgs p{dst_dev, src_dev, parent_dev, len_dev, B, width, n_pos, pos_bytes, slot, (slot + 256 * vec - 1) / (256 * vec)};      // chunks: the most of any form
-  if ((int64_t)n_layers * B * (double)p.chunks >= 2147483648.0) return fail(WF_E_CAPACITY, "%lld bytes in %d layers: more than 2^31 workgroups", (long long)all, n_layers);
+  ReorderArgs p{dst_dev, src_dev, parent_dev, len_dev, B, width, n_pos, pos_bytes, slot, (slot + 256 * vec - 1) / (256 * vec)};      // the most workgroups of any form
+  if ((int64_t)n_layers * B * (double)p.chunks >= (double)(1 << 24))
+    return fail(WF_E_CAPACITY, "%lld bytes in %d layers, moved %d at a time: more than 2^32 threads", (long long)all, n_layers, vec);
   const int64_t ls = (int64_t)n_layers * B;
   const hipStream_t s = (hipStream_t)hip_stream;
   if (vec == 16) launch_reorder<u32x4>(p, ls, s);

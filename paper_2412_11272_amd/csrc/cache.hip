@@ -98,7 +98,7 @@ template <> struct Stored<WF_DTYPE_F32> { typedef float type; };
 template <typename T, int CACHE>
 __global__ void __launch_bounds__(256) cache_write_kernel(CacheView c, const T *k, const T *v, int64_t ld, const int32_t *cu, const int32_t *row, int B,
                                                           int n_tokens) {
-  const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (t >= n_tokens) return;
   const int lane = threadIdx.x & 63, part = (lane & 7) * 8, units = 2 * c.n_heads;
   int64_t r = -1;
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheView c, const T *
       if (u < units) x[i] = load8((u & 1 ? v : k) + t * ld + (u >> 1) * 64 + part);
     }
     if (u0 == 0) {                          // behind the loads: they do not wait for it
-      r = token_row(cu, row, B, c.n_rows, t);
+      r = token_row(cu, row, B, c.n_rows, (int)t);
       if (r < 0) return;
     }
 #pragma unroll
@@ -155,10 +155,10 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheView c, const T *
 
 template <typename T, int CACHE>
 __global__ void __launch_bounds__(256) cache_read_kernel(CacheView c, T *out, const int32_t *cu, const int32_t *row, int B, int n_tokens) {
-  const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (t >= n_tokens) return;
   const int lane = threadIdx.x & 63, part = (lane & 7) * 8, units = 2 * c.n_heads;
-  const int64_t r = token_row(cu, row, B, c.n_rows, t);
+  const int64_t r = token_row(cu, row, B, c.n_rows, (int)t);
   if (r == -2) return;
   typedef typename Stored<CACHE>::type S;
   for (int u0 = 0; u0 < units; u0 += 8 * kBatch) {
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheView c, T *out, co
       }
       Eight<T> y;
       from_floats(f, y);
-      store8(out + ((int64_t)t * 2 + (u & 1)) * c.n_heads * 64 + (u >> 1) * 64 + part, y);
+      store8(out + (t * 2 + (u & 1)) * c.n_heads * 64 + (u >> 1) * 64 + part, y);
     }
   }
 }
@@ -232,6 +232,7 @@ int check_tokens(const wf_cache *c, const int32_t *cu, const int32_t *row, int32
   if (dtype != WF_DTYPE_F32 && dtype != WF_DTYPE_BF16) return host::fail(WF_E_INVALID_ARG, "dtype = %d", dtype);
   if (B < 1) return host::fail(WF_E_INVALID_ARG, "B = %d, need B >= 1", B);
   if (n_tokens < 0) return host::fail(WF_E_INVALID_ARG, "n_tokens = %d", n_tokens);
+  if (n_tokens >= 1 << 26) return host::fail(WF_E_CAPACITY, "n_tokens = %d (supported: below 2^26 a call)", n_tokens);      // 64 threads each, fewer than 2^32
   if (n_tokens == 0) return WF_OK;
   if (!cu || !row) return host::fail(WF_E_INVALID_ARG, "cu_dev or row_dev is NULL");
   return host::check_cache_memory(c);

@@ -302,7 +302,8 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
   };
 
   State st[NQ];
-  const float c = fabsf(p.scale) * 1.4426950408889634f;      // exp(s scale) = exp2(s c)
+  // exp(s scale) = exp2(s c); never 0, so that a key that is not seen stays at -infinity
+  const float c = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 0x1p-149f);
 
   // FREE: every row sees every key of the tile.
   auto compute = [&](const Tile &a, int tile, auto free) {
@@ -713,7 +714,7 @@ int wf_op_cache_attention(const wf_cache *cache, const wf_cache_query *query, vo
                      a.n_heads, a.n_heads / cache->n_heads, a.n_seqs, a.n_q_rows, a.max_q, a.max_len, a.mask_words, plan.chunks, plan.n_split, plan.split_keys, a.scale};
   int64_t groups = (int64_t)a.n_seqs * cache->n_heads * plan.n_split;
   if (plan.chunks > 1) groups = round_up(groups, 8) * plan.chunks;
-  if (groups >= (int64_t)1 << 31) return fail(WF_E_CAPACITY, "%lld workgroups", (long long)groups);
+  if (groups * plan.nw >= (int64_t)1 << 26) return fail(WF_E_CAPACITY, "%lld workgroups (supported: below 2^32 threads)", (long long)groups);
   const dim3 grid((uint32_t)groups);
   const hipStream_t s = (hipStream_t)hip_stream;
   if (a.dtype == WF_DTYPE_BF16) {

@@ -273,6 +273,40 @@ def test_what_a_row_does_not_see_does_not_reach_it(act, cdtype):
             assert np.abs(got[r, h] - ref).max() <= 2.0 ** -7 * size.max() + 300 * U * dots * size.max()
 
 
+@pytest.mark.parametrize("n_q", [1, 5, 20, 40])
+@pytest.mark.parametrize("act,cdtype", KINDS)
+def test_long_masked_sequences_split_over_workgroups(act, cdtype, n_q):
+    # the tail is masked, a hidden key of it is NaN, and one row sees nothing behind the common prefix; the prefix of the second sequence is empty
+    lens, since = [4001, 2500], [3910, 0]
+    rows, cu = [5, 4100], [0, n_q, 2 * n_q]
+    cache = _filled(6700, 1, cdtype, 48)
+    clean = _contents(cache)
+    rng = np.random.default_rng(49)
+    words = rng.integers(0, 1 << 32, (2 * n_q, 80), dtype=np.uint32)
+    words[:, 0] &= ~np.uint32(1 << 9)
+    words[0, :3] = 0
+    words[n_q] = 0                            # sees nothing at all
+    hidden = [rows[0] + since[0] + 9, rows[1] + 9]
+    for r in hidden:
+        if cdtype == F8:
+            cache.data.view(torch.uint8)[r] = 0x7f
+        else:
+            cache.data[r] = float("nan")
+    q, mask = _q(2 * n_q, 2, act, 50), torch.from_numpy(words.view(np.int32)).cuda()
+    got = _np(wf.op_cache_attention(cache, q, _i32(cu), _i32(rows), _i32(lens), n_q, 4100, mask=mask, mask_from=_i32(since))).reshape(2 * n_q, 2, 64)
+    assert np.isfinite(got).all() and not got[n_q].any()
+    qn = _np(q).reshape(2 * n_q, 2, 64)
+    for r in sorted({0, n_q - 1, n_q, 2 * n_q - 1}):
+        s = int(r >= n_q)
+        seen = D.visible(lens[s], words[r], since[s])
+        for h in range(2):
+            kv = clean[rows[s]:rows[s] + lens[s], 0]
+            ref, size, dots = D.attention(qn[r, h], kv[:, 0], kv[:, 1], 0.125, seen)
+            tol = (2 * 72 * U * dots + 2.0 ** -21 + (2.0 ** -16 if act == BF else 0.0) + (2 * lens[s] + 64) * U) * size * (1 + 2.0 ** -7) + \
+                (2.0 ** -8 if act == BF else U) * np.abs(ref) + 1e-37      # as in _check_attention
+            assert (np.abs(got[r, h] - ref) <= tol).all(), (r, h)
+
+
 def test_values_that_are_not_finite_reach_only_their_place():
     # a value of infinity in one place of a key that all rows see: that place alone is infinite
     cache = _filled(50, 1, BF, 18)
@@ -292,6 +326,41 @@ def test_lengths_and_rows_outside_their_bounds(act, cdtype):
     assert (out[2:5] == 0).all() and (out[5:] == 77).all()
     # more queries than max_q, and prefix sums that leave the buffer
     _check_attention(cache, _q(8, 1, act, 21), [0, 6, 20], [0, 3], [20, 30], 3, 40)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+@pytest.mark.parametrize("act,cdtype", KINDS)
+def test_attention_scales_of_any_sign(act, cdtype, scale):
+    cache = _filled(90, 1, cdtype, 40)
+    q = _q(20, 2, act, 41, spread=1.0)
+    mask = torch.from_numpy(np.random.default_rng(42).integers(0, 1 << 32, (20, 3), dtype=np.uint32).view(np.int32)).cuda()
+    _check_attention(cache, q, [0, 3, 20], [0, 7], [45, 77], 17, 80, scale=scale)
+    _check_attention(cache, q, [0, 3, 20], [0, 7], [45, 77], 17, 80, scale=scale, mask=mask)
+
+
+@pytest.mark.parametrize("n_seqs", [1, 300])
+def test_attention_over_nothing(n_seqs):
+    cache = _filled(64, 8, BF, 43)
+    q = _q(n_seqs, 8, BF, 44)
+    out = wf.op_cache_attention(cache, q, _i32(range(n_seqs + 1)), _i32([0] * n_seqs), _i32([9] * n_seqs), 1, 0)
+    assert not out.any()
+    assert wf.op_cache_attention(cache, q[:0], _i32([0, 0]), _i32([0]), _i32([5]), 1, 5).shape == (0, 512)
+
+
+@pytest.mark.parametrize("length", [5, 64, 65, 256, 257])
+@pytest.mark.parametrize("act,cdtype", KINDS)
+def test_attention_of_many_short_sequences(act, cdtype, length):
+    # enough sequences that a workgroup has one, two or four waves by the longest one
+    B, H = 160, 8
+    lens = [(length * (i % 7)) // 6 for i in range(B)]
+    rows = [(i * 37) % 900 for i in range(B)]
+    cache = _filled(1200, H, cdtype, 45)
+    cu = list(range(B + 1))
+    some = {0, 1, 6, 40, 101, 159}
+    _check_attention(cache, _q(B, H, act, 46), cu, rows, lens, 1, length, heads=[0, 7], some_rows=some)
+    words = np.random.default_rng(47).integers(0, 1 << 32, (B, 3), dtype=np.uint32)
+    _check_attention(cache, _q(B, H, act, 46), cu, rows, lens, 1, length, heads=[0, 7], some_rows=some, mask=torch.from_numpy(words.view(np.int32)).cuda(),
+                     since=[max(0, n - 70) for n in lens])
 
 
 def test_attention_strides_and_shapes():

@@ -57,6 +57,7 @@ def test_write_and_read_arguments():
         assert _write(c, **bad) == _read(c, **bad) == wf.WF_E_INVALID_ARG, bad
     for bad in (dict(ld=255), dict(n=5, k=None), dict(n=5, v=None), dict(n=5, k=P + 8), dict(n=5, v=P + 2), dict(n=5, ld=260)):
         assert _write(c, **bad) == wf.WF_E_INVALID_ARG, bad
+    assert _write(c, n=1 << 26) == _read(c, n=1 << 26) == wf.WF_E_CAPACITY
     assert _read(c, n=5, out=None) == _read(c, n=5, out=P + 4) == wf.WF_E_INVALID_ARG
 
 
@@ -83,6 +84,11 @@ def test_attention_arguments():
     assert call(_cache(dtype=wf.WF_DTYPE_F32, exps_dev=None)) == wf.WF_E_INVALID_ARG       # bf16 queries over a fp32 cache
     assert call(n_seqs=1 << 20, n_q_rows=1 << 20, max_q=1 << 20) == wf.WF_E_CAPACITY
     assert L.wf_cache_attention_workspace(C.byref(c), C.byref(_query())) >= 0
+    long = _query(n_q_rows=2, max_len=1 << 20)                      # split over workgroups: the parts need room
+    need = L.wf_cache_attention_workspace(C.byref(c), C.byref(long))
+    assert need > 0 and call(n_q_rows=2, max_len=1 << 20) == wf.WF_E_INVALID_ARG
+    assert call(n_q_rows=2, max_len=1 << 20, workspace_dev=P, workspace_bytes=need - 1) == wf.WF_E_CAPACITY
+    assert call(n_q_rows=2, max_len=1 << 20, workspace_dev=P + 8, workspace_bytes=need) == wf.WF_E_INVALID_ARG
 
 
 def _step(**kw):
@@ -108,6 +114,10 @@ def test_beam_select_arguments():
     assert call(B=1 << 20) == wf.WF_E_CAPACITY
 
 
+def _step_over(**kw):
+    return wf.lib().wf_beam_select_workspace(C.byref(_step(**kw)))
+
+
 def test_beam_reorder_arguments():
     def call(dst=P, src=P, parent=P, length=None, B=2, width=3, layers=0, n_pos=10, pos_bytes=16):
         return wf.lib().wf_op_beam_reorder(dst, src, parent, length, B, width, layers, n_pos, pos_bytes, None)
@@ -117,7 +127,8 @@ def test_beam_reorder_arguments():
                 dict(layers=1, src=None), dict(layers=1, parent=None), dict(layers=1, src=P + 2 * 3 * 160 - 1), dict(layers=1, src=P - 16),
                 dict(layers=2, n_pos=1 << 40, pos_bytes=1 << 40)):
         assert call(**bad) == wf.WF_E_INVALID_ARG, bad
-    assert call(layers=2, n_pos=1 << 40) == wf.WF_E_CAPACITY
+    assert call(layers=2, n_pos=1 << 40) == call(layers=1, n_pos=1 << 34, pos_bytes=1) == wf.WF_E_CAPACITY
+    assert _step_over(n_vocab=(1 << 28) + 1) == wf.WF_E_CAPACITY
 
 
 def test_binding_refuses_host_tensors():
