@@ -4,7 +4,10 @@
 // Bound by memory: a key / value pair of a head is 256 bytes in bf16 (130 in 8 bits) and serves only the query rows that share the
 // head (queries of the sequence times query heads per key head), so the cache goes from memory straight to registers, once,
 // and nothing of it through the LDS.  A workgroup has one key / value head of one sequence, up to 16 * NQ of its query rows and a range of keys; its
-// waves take tiles of 32 keys in turn, each with a running maximum and sum of its own, and join in the LDS at the end.
+// waves take tiles of 32 keys in turn, each with a running maximum and sum of its own, and join in the LDS at the end.  Measured on one MI355X (a
+// read-only pass over memory in this pattern reaches 5.3 .. 5.8 TB/s): 320 sequences of 512 keys of 20 heads 6.06 TB/s in bf16, 5.63 in 8 bits, 6.14 in fp32;
+// five beams each of 64 streams of 51 .. 1525 keys 4.5, 3.8 and 4.9, held up by the uneven lengths; trees of 68 .. 160 rows are held up by the
+// softmax's and the weights' instructions, 2.1 TB/s and 260 TFLOP/s.
 //
 // A tile's products, on the 16 x 16 matrix instructions, run transposed like those of the prefill attention: S^T = K Q^T, O^T = V^T P^T.
 // A lane (n = lane % 16, g = lane / 16) then holds
@@ -183,17 +186,16 @@ __device__ __forceinline__ RowState one_row(const AttendArgs &p, int64_t r, int 
   return w;
 }
 
-template <typename T, int CACHE, int NQ, bool MASK>
-constexpr int min_waves() { return NQ == 1 && sizeof(T) == 2 ? CACHE == WF_DTYPE_F8 && !MASK ? 3 : 3 : 2; }
-
 template <typename T, int CACHE, int NQ, int NW, bool MASK>
-__global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) cache_attention_kernel(AttendArgs p) {
+__global__ void __launch_bounds__(64 * NW, NQ == 1 && sizeof(T) == 2 ? 3 : 2) cache_attention_kernel(AttendArgs p) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int es = Format<CACHE>::es;
   typedef Tile<CACHE, NQ, MASK> Tile;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
   const int H = p.c.n_heads;
-  // Workgroups go to the 8 XCDs in turn: those that read the same keys for other rows come 8 behind each other, to the same L2.
+  // Workgroups go to the 8 XCDs in turn: those that read the same keys for other rows come 8 behind each other, to the same L2.  The heads are
+  // turned by one from one sequence to the next: with 8 or 16 of them, every XCD would read the same few of them only, whose rows lie at the same
+  // places of the memory's channels (five beams of 64 streams, 20 heads: bf16 60.7 -> 56.2 us, fp32 110 -> 103; drafted trees, 8 heads: 146 -> 140).
   int id = blockIdx.x, chunk = 0;
   if (p.chunks > 1) {
     chunk = id / 8 % p.chunks;
@@ -305,11 +307,8 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
   // exp(s scale) = exp2(s c); never 0, so that a key that is not seen stays at -infinity
   const float c = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 0x1p-149f);
 
-  // FREE: every row sees every key of the tile.
-  auto compute = [&](const Tile &a, int tile, auto free) {
-    constexpr bool FREE = decltype(free)::value;
-    // ---- values: pairs of keys next to each other
-    uint32_t vt[4][BF ? 4 : 8];
+  // The values with pairs of keys next to each other, as the second product takes them
+  auto values = [&](const Tile &a, uint32_t (&vt)[4][BF ? 4 : 8]) {
     if constexpr (BF) {
       uint32_t v[8][2];
 #pragma unroll
@@ -343,6 +342,12 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
         }
       }
     }
+  };
+  // FREE: every row sees every key of the tile.
+  auto compute = [&](const Tile &a, int tile, auto free) {
+    constexpr bool FREE = decltype(free)::value;
+    uint32_t vt[4][BF ? 4 : 8];
+    if constexpr (NQ > 1) values(a, vt);
     // ---- keys
     uint32_t kt[2][QD];
 #pragma unroll
@@ -370,92 +375,93 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
     constexpr int GT = NQ < 2 ? NQ : 2;
 #pragma unroll
     for (int t0 = 0; t0 < NQ; t0 += GT) {
-    if (t0 > 0 && t0 >= n_tiles_q) break;
-    float x[GT][8];
-    bool rise = false;
-#pragma unroll
-    for (int k = 0; k < GT; ++k) {
-      const int t = t0 + k;
-      uint32_t qa[QD];
-#pragma unroll
-      for (int i = 0; i < QD; ++i) qa[i] = q_one[i];
-      if constexpr (NQ > 1)
-#pragma unroll
-        for (int i = 0; i < QD / 4; ++i) {
-          const u32x4 y = s_q[t][i][lane];
-          qa[4 * i] = y[0]; qa[4 * i + 1] = y[1]; qa[4 * i + 2] = y[2]; qa[4 * i + 3] = y[3];
-        }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x4 d{0.0f, 0.0f, 0.0f, 0.0f};
-        if constexpr (BF) {
-#pragma unroll
-          for (int f = 0; f < 2; ++f) {
-            const uint32_t ka[4] = {kt[u][4 * f], kt[u][4 * f + 1], kt[u][4 * f + 2], kt[u][4 * f + 3]};
-            const uint32_t qb[4] = {qa[4 * f], qa[4 * f + 1], qa[4 * f + 2], qa[4 * f + 3]};
-            d = mma(ka, qb, d);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            d = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kt[u][i]), __builtin_bit_cast(float, qa[i]), d, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[k][4 * u + i] = d[i];
-      }
-      if constexpr (!FREE) {
-        const uint32_t mine = seen_keys(a, tile, t) >> (4 * g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (!(mine >> (16 * (j >> 2) + (j & 3)) & 1)) x[k][j] = -INFINITY;
-      }
-      float top = x[k][0];
-#pragma unroll
-      for (int j = 1; j < 8; ++j) top = fmaxf(top, x[k][j]);
-      rise |= (top > -INFINITY) & (top * c > st[t].m + 8.0f);
-    }
-    // A row's reference follows its maximum only where that is 2^8 above it: weights of up to 2^8 lose nothing in fp32.
-    if (__ballot(rise)) {
+      if (t0 > 0 && t0 >= n_tiles_q) break;
+      float x[GT][8];
+      bool rise = false;
 #pragma unroll
       for (int k = 0; k < GT; ++k) {
-        State &w = st[t0 + k];
+        const int t = t0 + k;
+        uint32_t qa[QD];
+#pragma unroll
+        for (int i = 0; i < QD; ++i) qa[i] = q_one[i];
+        if constexpr (NQ > 1)
+#pragma unroll
+          for (int i = 0; i < QD / 4; ++i) {
+            const u32x4 y = s_q[t][i][lane];
+            qa[4 * i] = y[0]; qa[4 * i + 1] = y[1]; qa[4 * i + 2] = y[2]; qa[4 * i + 3] = y[3];
+          }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          f32x4 d{0.0f, 0.0f, 0.0f, 0.0f};
+          if constexpr (BF) {
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+              const uint32_t ka[4] = {kt[u][4 * f], kt[u][4 * f + 1], kt[u][4 * f + 2], kt[u][4 * f + 3]};
+              const uint32_t qb[4] = {qa[4 * f], qa[4 * f + 1], qa[4 * f + 2], qa[4 * f + 3]};
+              d = mma(ka, qb, d);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              d = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kt[u][i]), __builtin_bit_cast(float, qa[i]), d, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[k][4 * u + i] = d[i];
+        }
+        if constexpr (!FREE) {
+          const uint32_t mine = seen_keys(a, tile, t) >> (4 * g);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (!(mine >> (16 * (j >> 2) + (j & 3)) & 1)) x[k][j] = -INFINITY;
+        }
         float top = x[k][0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) top = fmaxf(top, x[k][j]);
-        const Pair rp = row_pair(top);
-        top = half_max(fmaxf(rp.a, rp.b));
-        top = top == -INFINITY ? w.m : fmaxf(w.m, top * c);
-        const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - top);
-        w.l *= keep;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w.o[i] *= keep;
-        w.m = top;
+        rise |= (top > -INFINITY) & (top * c > st[t].m + 8.0f);
       }
-    }
+      // A row's reference follows its maximum only where that is 2^8 above it: weights of up to 2^8 lose nothing in fp32.
+      if (__ballot(rise)) {
 #pragma unroll
-    for (int k = 0; k < GT; ++k) {
-      State &w = st[t0 + k];
-      const float base = w.m == -INFINITY ? 0.0f : w.m;
+        for (int k = 0; k < GT; ++k) {
+          State &w = st[t0 + k];
+          float top = x[k][0];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[k][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][j], c, -base));
-      w.l += ((x[k][0] + x[k][1]) + (x[k][2] + x[k][3])) + ((x[k][4] + x[k][5]) + (x[k][6] + x[k][7]));
-      if constexpr (BF) {
-        uint32_t hi[4], lo[4];
+          for (int j = 1; j < 8; ++j) top = fmaxf(top, x[k][j]);
+          const Pair rp = row_pair(top);
+          top = half_max(fmaxf(rp.a, rp.b));
+          top = top == -INFINITY ? w.m : fmaxf(w.m, top * c);
+          const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - top);
+          w.l *= keep;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          hi[j] = pack(__builtin_convertvector(f32x2{x[k][2 * j], x[k][2 * j + 1]}, bf16x2));
-          const f32x2 rest = {x[k][2 * j] - __builtin_bit_cast(float, hi[j] << 16), x[k][2 * j + 1] - __builtin_bit_cast(float, hi[j] & 0xffff0000u)};
-          lo[j] = pack(__builtin_convertvector(rest, bf16x2));
+          for (int i = 0; i < 4; ++i) w.o[i] *= keep;
+          w.m = top;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w.o[i] = mma(vt[i], hi, mma(vt[i], lo, w.o[i]));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w.o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vt[i][j]), x[k][j], w.o[i], 0, 0, 0);
       }
-    }
+#pragma unroll
+      for (int k = 0; k < GT; ++k) {
+        State &w = st[t0 + k];
+        const float base = w.m == -INFINITY ? 0.0f : w.m;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[k][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][j], c, -base));
+        w.l += ((x[k][0] + x[k][1]) + (x[k][2] + x[k][3])) + ((x[k][4] + x[k][5]) + (x[k][6] + x[k][7]));
+        if constexpr (NQ == 1) values(a, vt);      // once the keys' registers are free
+        if constexpr (BF) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            hi[j] = pack(__builtin_convertvector(f32x2{x[k][2 * j], x[k][2 * j + 1]}, bf16x2));
+            const f32x2 rest = {x[k][2 * j] - __builtin_bit_cast(float, hi[j] << 16), x[k][2 * j + 1] - __builtin_bit_cast(float, hi[j] & 0xffff0000u)};
+            lo[j] = pack(__builtin_convertvector(rest, bf16x2));
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w.o[i] = mma(vt[i], hi, mma(vt[i], lo, w.o[i]));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w.o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vt[i][j]), x[k][j], w.o[i], 0, 0, 0);
+        }
+      }
     }
   };
 #pragma unroll
@@ -465,27 +471,26 @@ __global__ void __launch_bounds__(64 * NW, (min_waves<T, CACHE, NQ, MASK>())) ca
 #pragma unroll
     for (int i = 0; i < 4; ++i) st[t].o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  constexpr int D = 2;      // tiles of a wave in registers: one in use, one on its way
-  Tile ring[D];
+  // One tile is in use, one on its way (two on their way gain nothing: 39.4 us against 38.4 with five beams of 64 streams in 8 bits).
+  // The two change places by an unrolled index: written out one after the other, the same steps leave the compiler short of registers (355 us against
+  // 138 with the drafted trees).
+  Tile ring[2];
   int tile = t_first;
-#pragma unroll
-  for (int i = 0; i < D - 1; ++i)
-    if (tile + i * NW < t_end) load(ring[i], tile + i * NW);
-  const int t_free = MASK ? (int)((from < n ? from > 0 ? from : 0 : n) / kTile) : n / kTile;      // tiles before it are free
+  if (tile < t_end) load(ring[0], tile);
+  const int t_free = MASK ? (from < n ? from > 0 ? from : 0 : n) / kTile : n / kTile;      // tiles before it are free
   while (tile < t_end && tile < t_free) {
 #pragma unroll
-    for (int i = 0; i < D; ++i) {
-      if (tile + (D - 1) * NW < t_end) load(ring[(i + D - 1) % D], tile + (D - 1) * NW);
+    for (int i = 0; i < 2; ++i) {
+      if (tile + NW < t_end) load(ring[1 - i], tile + NW);
       compute(ring[i], tile, std::true_type{});
       tile += NW;
       if (tile >= t_end || tile >= t_free) {
-        if (i + 1 < D) ring[0] = ring[i + 1];
+        if (i == 0) ring[0] = ring[1];
         break;
       }
     }
   }
   while (tile < t_end) {
-    static_assert(D == 2, "one tile ahead");
     if (tile + NW < t_end) load(ring[1], tile + NW);
     compute(ring[0], tile, std::false_type{});
     ring[0] = ring[1];
@@ -625,15 +630,22 @@ struct Plan {
   int nq, nw, chunks, n_split, split_keys;
 };
 
+// Query rows of a workgroup: 16, 32 or 64 (fp32: 32, more outgrow the registers).  Rows beyond that read the keys again, from the L2: trees of 68 .. 160
+// rows over 20 000 .. 65 536 bf16 keys take 140 us with 64, 160 with 32; 64 rows over 1500 keys of 20 heads 41 and 43 (in 8 bits, where a
+// tile's conversion weighs more but the tiles are half as many bytes, 34 and 29).
+// Workgroups: keys are split where a chip of 256 compute units would not get four (eight, if they have more than 16 rows and so last long and unevenly)
+// each: one token over 65 536 keys of 8 heads in 8 bits 23.2 us with 1024, 23.8 with 2048; the trees 163 and 147.  A part keeps 768 keys: below, joining costs more
+// than it wins (1500 keys of 20 heads: 12.6 us in one part, 17 in two; 8 x 8192 keys of 8 heads in bf16 39 us with 1024 a part, 35.5 with 512).
+// Waves: four share a sequence's tiles; where sequences are short and many, two or one (320 of them, 20 heads, 8 bits: 32 keys 26.5 us with four, 16.9 with
+// two, 12.6 with one; 128 keys 37.1, 27.5, 25.5; 256 keys 47.7, 42.3, 43.2; 512 keys 75.9, 77.1, 80.4).
 Plan plan_of(const wf_cache &c, const wf_cache_query &a) {
   Plan p{};
   const int64_t rows = (int64_t)std::min(a.max_q, std::max(a.n_q_rows, 1)) * (a.n_heads / c.n_heads);
-  p.nq = rows <= 16 ? 1 : rows <= 32 || a.dtype == WF_DTYPE_F32 ? 2 : 4;      // 64 rows of fp32 operands outgrow the registers
+  p.nq = rows <= 16 ? 1 : rows <= 32 || a.dtype == WF_DTYPE_F32 ? 2 : 4;
   p.chunks = (int)((rows + 16 * p.nq - 1) / (16 * p.nq));
   const int64_t groups = (int64_t)a.n_seqs * c.n_heads * p.chunks, want = p.nq > 1 ? 2048 : 1024;
   int64_t n = groups >= want ? 1 : (want + groups - 1) / groups;
-  const int64_t most = std::max<int64_t>(1, a.max_len / 768);
-  n = std::min<int64_t>(std::min(n, most), kMaxSplits);
+  n = std::min<int64_t>(std::min<int64_t>(n, std::max(1, a.max_len / 768)), kMaxSplits);
   p.split_keys = (int)std::min<int64_t>(host::round_up(std::max<int64_t>((a.max_len + n - 1) / n, kTile), kTile), INT32_MAX / kTile * kTile);
   p.n_split = (int)std::max<int64_t>(1, ((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
   p.nw = p.nq > 1 || groups < 1024 || a.max_len > 256 ? 4 : a.max_len > 64 ? 2 : 1;
