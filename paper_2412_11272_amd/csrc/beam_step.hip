@@ -102,8 +102,9 @@ template <> struct Values<__bf16> {
 // One wave per part: read once, into registers.  The width best are among the values that reach the width-th largest of the 64 lanes'
 // maxima (so many lanes do, each with one value at least); a bisection over the upper half of the bits finds a bound just below it,
 // usually a handful of values pass, and these are ranked by comparing each with each.  Where more than 64 pass (equal values, few finite
-// ones) the best are taken out one by one.  64 x 5 beams over 51 866 tokens, 66 MB of fp32: 13 us here and 6 for the merge (scanning a row once for each
-// candidate took 418); the memory's share would be 11: the rest is instructions, bf16 logits take 15 and 6.
+// ones) the best are taken out one by one.  64 x 5 beams over 51 866 tokens, 66 MB of fp32: 15 us here and 6 for the merge (scanning a row once for each
+// candidate took 418); the memory's share would be 11: some 460 vector instructions a part take
+// the rest, and bf16 logits 18 us in all.
 template <typename T>
 __global__ void __launch_bounds__(256) beam_parts_kernel(SelectArgs p) {
   constexpr int N = Values<T>::N, CH = 32 / N;
