@@ -492,7 +492,7 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  * step to step (lengths, rows, parents) is read from device memory, so that one captured graph serves every step; the host arguments are
  * upper bounds.  Device values that lie outside their bounds never lead to an access outside the buffers: such rows or slots are
  * left out, as stated with each operator.  All work of a call is ordered on its stream; two calls may overlap if their outputs and
- * workspaces are their own.
+ * workspaces are their own.  Sources, caches and outputs of one call must not overlap unless it is said below.
  *
  * A cache holds keys and values of n_heads heads of size 64 in n_rows rows:
  *   WF_DTYPE_F32, WF_DTYPE_BF16   data_dev [n_rows, 2 * 64 * n_heads]: the keys of all heads, then the values (a layer of wf_cross_kv's or
@@ -521,7 +521,8 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *                     ldq, ldo in elements; q_dev, out_dev and both strides in bytes are multiples of 16 bytes.  max_q and max_len bound the
  *                     queries and keys of a sequence: len_dev[s] counts as max_len where it is larger, and as what the cache has from
  *                     row_dev[s] on; rows of a sequence behind its first max_q, and rows behind the last sequence, are left as they were.
- *                     workspace_dev: at least wf_cache_attention_workspace(..) bytes (0: may be NULL), aligned to 16, of any content.
+ *                     workspace_dev: at least wf_cache_attention_workspace(..) bytes (0: may be NULL), aligned to 16, of any content.  How the keys are
+ *                     shared out, and with it the last bits of a result, goes by the bounds and counts of the call, not by the lengths.
  * wf_op_beam_select   one step of a beam search, per stream s of B with n_in[s] beams (DEVICE int32 [B]; NULL: width; clamped to 0 .. width):
  *                     candidates (b, t) of all beams b and tokens t with total(b, t) = score_in[s, b] + logits[s, b, t] - log sum exp
  *                     logits[s, b, :], in 64 bits.  The n_out[s] (NULL: width) best come out, best first: tokens of one beam by

@@ -802,7 +802,9 @@ class Cache:
         import torch
         shape = data.shape
         f8 = data.dtype == torch.float8_e4m3fn
-        self.device = _here(data, "data")
+        self.device = data.get_device()          # a call checks that it is the current one
+        if self.device < 0:
+            raise ValueError(f"data is on {data.device}, need a CUDA device")
         if not data.is_contiguous() or (len(shape) != 4 or shape[2] != 2 or shape[3] != 64 if f8 else len(shape) != 2 or shape[1] % 128):
             raise ValueError(f"data: {tuple(shape)} with strides {data.stride()}, need [n_rows, 128 n_heads] or, in 8 bits, [n_rows, n_heads, 2, 64]")
         n_rows, n_heads = shape[0], shape[1] if f8 else shape[1] // 128

@@ -103,8 +103,7 @@ template <> struct Values<__bf16> {
 // maxima (so many lanes do, each with one value at least); a bisection over the upper half of the bits finds a bound just below it,
 // usually a handful of values pass, and these are ranked by comparing each with each.  Where more than 64 pass (equal values, few finite
 // ones) the best are taken out one by one.  64 x 5 beams over 51 866 tokens, 66 MB of fp32: 15 us here and 6 for the merge (scanning a row once for each
-// candidate took 418); the memory's share would be 11: some 460 vector instructions a part take
-// the rest, and bf16 logits 18 us in all.
+// candidate took 418).  The memory's share would be 11, some 460 vector instructions a part take the rest; bf16 logits take 18 us in all.
 template <typename T>
 __global__ void __launch_bounds__(256) beam_parts_kernel(SelectArgs p) {
   constexpr int N = Values<T>::N, CH = 32 / N;
@@ -403,6 +402,7 @@ int wf_op_beam_select(const wf_beam_step *a, void *hip_stream) {
   if (need < 0) return (int)need;
   if (!a->logits_dev || !a->score_in_dev || !a->token_out_dev || !a->parent_out_dev || !a->score_out_dev)
     return fail(WF_E_INVALID_ARG, "logits_dev, score_in_dev or one of the outputs is NULL");
+  if ((uintptr_t)a->logits_dev % (a->dtype == WF_DTYPE_BF16 ? 2 : 4)) return fail(WF_E_INVALID_ARG, "logits_dev is not aligned to its type");
   if (a->ld < a->n_vocab) return fail(WF_E_INVALID_ARG, "ld = %lld, need at least n_vocab = %d", (long long)a->ld, a->n_vocab);
   if ((a->done_in_dev != nullptr) != (a->done_out_dev != nullptr)) return fail(WF_E_INVALID_ARG, "done_in_dev and done_out_dev go together");
   if (a->done_in_dev && (a->eos < 0 || a->eos >= a->n_vocab)) return fail(WF_E_INVALID_ARG, "eos = %d outside [0, %d)", a->eos, a->n_vocab);

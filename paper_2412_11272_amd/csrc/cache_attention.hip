@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(64 * NW, NQ == 1 && sizeof(T) == 2 ? 3 : 2) ca
 
   // ---- the waves' parts meet
   constexpr int kRow = 68;       // floats of a row in the LDS: 64 and room against bank conflicts
-  __shared__ float s_o[NW][16][kRow];
+  __shared__ __attribute__((aligned(16))) float s_o[NW][16][kRow];
   __shared__ float s_m[NW][16], s_l[NW][16];
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {

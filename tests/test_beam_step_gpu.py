@@ -138,6 +138,32 @@ def test_select_may_overwrite_its_own_scores():
     assert torch.equal(t2, tok) and torch.equal(p2, par) and torch.equal(sc, score) and torch.equal(done, dout)
 
 
+def test_a_workspace_of_the_callers_own():
+    import ctypes as C
+    x, sc = _logits(3, 5, 9001, 12), torch.tensor(_scores(3, 5, 12).astype(np.float32), device="cuda")
+    want = wf.op_beam_select(x, sc)
+    need = wf.lib().wf_beam_select_workspace(C.byref(wf.WfBeamStep(dtype=wf.WF_DTYPE_F32, B=3, width=5, n_vocab=9001)))
+    room = torch.full((need + 64,), 0xff, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        got = wf.op_beam_select(x, sc, workspace=room[:need])
+        assert all(torch.equal(a, b) for a, b in zip(got[:3], want[:3]))
+    assert (room[need:] == 0xff).all()
+    with pytest.raises(wf.WfError) as e:
+        wf.op_beam_select(x, sc, workspace=room[:need - 16])
+    assert e.value.code == wf.WF_E_CAPACITY
+
+
+def test_select_on_another_stream_than_the_current_one():
+    x, sc = _logits(8, 5, 20000, 13), torch.tensor(_scores(8, 5, 13).astype(np.float32), device="cuda")
+    want = wf.op_beam_select(x, sc)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [wf.op_beam_select(x, sc, stream=s.cuda_stream) for _ in range(5) for s in streams]
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g[:3], want[:3]))
+
+
 # ---- reordering -------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("inside", [(96, "bf16"), (5, "u8"), (3, "f32"), (64, "u8")], ids=str)

@@ -420,6 +420,31 @@ def test_one_sequence_of_a_cache_beyond_32_bit_offsets(act, cdtype):
             assert (np.abs(_np(b)[r, 64 * h:64 * h + 64] - ref) <= (2.0 ** -8 if act == BF else 0) * np.abs(ref) + (2.0 ** -12 + 2.0 ** -16) * size).all()
 
 
+@pytest.mark.parametrize("heads", [(40, 1), (96, 2)], ids=str)
+@pytest.mark.parametrize("act,cdtype", KINDS)
+def test_attention_of_large_head_groups(act, cdtype, heads):
+    Hq, H = heads
+    cache = _filled(180, H, cdtype, 51)
+    _check_attention(cache, _q(6, Hq, act, 52), [0, 1, 5], [3, 60], [57, 120], 4, 120, heads=[0, 1, Hq // H - 1, Hq - 1])
+
+
+def test_a_workspace_of_the_callers_own():
+    import ctypes as C
+    cache, q = _filled(6000, 2, F8, 53), _q(4, 4, BF, 54)
+    args = (_i32([0, 1, 4]), _i32([0, 1000]), _i32([6000, 5000]), 3, 6000)
+    want = wf.op_cache_attention(cache, q, *args)
+    a = wf.WfCacheQuery(dtype=wf.WF_DTYPE_BF16, n_heads=4, n_seqs=2, n_q_rows=4, max_q=3, max_len=6000, scale=0.125)
+    need = wf.lib().wf_cache_attention_workspace(C.byref(cache._c), C.byref(a))
+    assert need > 0
+    room = torch.full((need + 64,), 0xff, dtype=torch.uint8, device="cuda")        # of any content, and not written past its end
+    for _ in range(3):
+        assert torch.equal(wf.op_cache_attention(cache, q, *args, workspace=room[:need]), want)
+    assert (room[need:] == 0xff).all()
+    with pytest.raises(wf.WfError) as e:
+        wf.op_cache_attention(cache, q, *args, workspace=room[:need - 16])
+    assert e.value.code == wf.WF_E_CAPACITY
+
+
 def test_a_captured_step_follows_the_lengths_on_the_device():
     # one graph: the new token's row is written, then attended to; replayed while lengths, rows and inputs change
     H, cap, B = 4, 120, 3

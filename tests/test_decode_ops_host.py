@@ -109,7 +109,7 @@ def test_beam_select_arguments():
     for bad in (dict(dtype=wf.WF_DTYPE_F8), dict(B=0), dict(width=0), dict(width=33), dict(n_vocab=0), dict(logits_dev=None), dict(score_in_dev=None),
                 dict(token_out_dev=None), dict(parent_out_dev=None), dict(score_out_dev=None), dict(ld=99), dict(done_in_dev=P), dict(done_out_dev=P),
                 dict(done_in_dev=P, done_out_dev=P, eos=100), dict(done_in_dev=P, done_out_dev=P, eos=-1), dict(workspace_dev=None),
-                dict(workspace_dev=P + 8)):
+                dict(workspace_dev=P + 8), dict(logits_dev=P + 2), dict(logits_dev=P + 1, dtype=wf.WF_DTYPE_BF16)):
         assert call(**{**dict(workspace_bytes=0), **bad}) == wf.WF_E_INVALID_ARG, bad
     assert call(B=1 << 20) == wf.WF_E_CAPACITY
 
