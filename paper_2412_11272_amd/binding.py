@@ -863,7 +863,7 @@ def op_cache_attention(cache: Cache, q, cu_q, rows, lens, max_q: int, max_len: i
     if cols % 64:
         raise ValueError(f"q: {cols} columns, need 64 for each head")
     if out is None:       # rows that belong to no sequence are not written
-        out, ldo = _empty(q.shape, q.dtype, q, stream), cols
+        out, ldo = _like(q, q.dtype, stream) if q.is_contiguous() else _empty(q.shape, q.dtype, q, stream), cols
     else:
         n_out, cols_out, ldo = _rows_2d(out, here, "out")
         if n_out != n or cols_out != cols or out.dtype != q.dtype:

@@ -137,6 +137,14 @@ def _contents(cache):
     return _np(cache.data.float()) * 2.0 ** (e - 127)
 
 
+def _tolerance(act, n, ref, size, dots):
+    # A logit is off by 72 half steps of its 64 products' sum (its additions, the scale and the difference), a weight by twice that, by its
+    # exponential's 2^-21 and, next to a bf16 operand, by the 2^-16 that two bf16 parts leave; sums of n terms by n half steps, numerator and
+    # denominator; the result by its last rounding.
+    tol = (2 * 72 * U * dots + 2.0 ** -21 + (2.0 ** -16 if act == BF else 0.0) + (2 * n + 64) * U) * size
+    return tol * (1 + 2.0 ** -7) + (2.0 ** -8 if act == BF else U) * np.abs(ref) + 1e-37
+
+
 def _check_attention(cache, q, cu, rows, lens, max_q, max_len, mask=None, since=None, scale=0.125, call=None, heads=None, some_rows=None):
     """The call's output against the definition; untouched rows must keep the marker.  Returns the output."""
     T, Hq = q.shape[0], q.shape[1] // 64
@@ -160,11 +168,7 @@ def _check_attention(cache, q, cu, rows, lens, max_q, max_len, mask=None, since=
                 hk = h // (Hq // cache.n_heads)
                 block = kv[rows[s]:rows[s] + n, hk] if n else np.zeros((0, 2, 64))
                 ref, size, dots = D.attention(qn[r, h], block[:, 0], block[:, 1], scale, seen)
-                # a logit is off by 72 half steps of its 64 products' sum (its additions, the scale and the difference), a weight by
-                # twice that, by its exponential's 2^-21 and, next to a bf16 operand, by the 2^-16 that two bf16 parts leave; sums of n terms
-                # by n half steps, numerator and denominator; the result by its last rounding.
-                tol = (2 * 72 * U * dots + 2.0 ** -21 + (2.0 ** -16 if q.dtype == BF else 0.0) + (2 * n + 64) * U) * size
-                tol = tol * (1 + 2.0 ** -7) + (2.0 ** -8 if q.dtype == BF else U) * np.abs(ref) + 1e-37
+                tol = _tolerance(q.dtype, n, ref, size, dots)
                 err = np.abs(got[r, h] - ref)
                 worst = max(worst, float((err / tol).max()))
                 assert (err <= tol).all(), (s, r, h, float((err / tol).max()))
@@ -270,7 +274,7 @@ def test_what_a_row_does_not_see_does_not_reach_it(act, cdtype):
         seen = D.visible(lens[s], mask[r], 0)
         for h in range(4):
             ref, size, dots = D.attention(qn[r, h], clean[rows[s]:rows[s] + lens[s], h // 2, 0], clean[rows[s]:rows[s] + lens[s], h // 2, 1], 0.125, seen)
-            assert np.abs(got[r, h] - ref).max() <= 2.0 ** -7 * size.max() + 300 * U * dots * size.max()
+            assert (np.abs(got[r, h] - ref) <= _tolerance(act, lens[s], ref, size, dots)).all(), (r, h)
 
 
 @pytest.mark.parametrize("n_q", [1, 5, 20, 40])
@@ -302,9 +306,7 @@ def test_long_masked_sequences_split_over_workgroups(act, cdtype, n_q):
         for h in range(2):
             kv = clean[rows[s]:rows[s] + lens[s], 0]
             ref, size, dots = D.attention(qn[r, h], kv[:, 0], kv[:, 1], 0.125, seen)
-            tol = (2 * 72 * U * dots + 2.0 ** -21 + (2.0 ** -16 if act == BF else 0.0) + (2 * lens[s] + 64) * U) * size * (1 + 2.0 ** -7) + \
-                (2.0 ** -8 if act == BF else U) * np.abs(ref) + 1e-37      # as in _check_attention
-            assert (np.abs(got[r, h] - ref) <= tol).all(), (r, h)
+            assert (np.abs(got[r, h] - ref) <= _tolerance(act, lens[s], ref, size, dots)).all(), (r, h)
 
 
 def test_values_that_are_not_finite_reach_only_their_place():
