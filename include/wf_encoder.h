@@ -500,15 +500,15 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *   WF_DTYPE_F8   data_dev [n_rows, n_heads, 2, 64] e4m3 (OCP, no infinity): of each head 64 key values, then 64 values; exps_dev uint8
  *                 [2 * n_heads, n_rows]: entry (2 h, r) for the keys, (2 h + 1, r) for the values of head h in row r.  A stored q stands for
  *                 q * 2^(exponent - 127).
- * data_dev is aligned to 16 bytes.  A sequence is a range of consecutive rows; where the ranges of two sequences overlap, writing both in
- * one call leaves either's values there.
+ * data_dev is aligned to 16 bytes.  A sequence is a range of consecutive rows.  Ranges may overlap where they are read; what rows hold that two
+ * sequences of one call write is not defined.
  *
  * wf_op_cache_write   token t of sequence s, cu_dev[s] <= t < cu_dev[s + 1] (DEVICE int32 [B+1] prefix sums), goes to row
  *                     row_dev[s] + t - cu_dev[s] (DEVICE int32 [B]).  k_dev, v_dev: [n_tokens, 64 * n_heads] of dtype f32 or bf16, row stride
  *                     ld elements (>= 64 * n_heads; both pointers and ld * element size multiples of 16 bytes).  F8: each head's key and
  *                     value vector gets the smallest power of two 2^e >= 2^-127 with max|x| <= 448 * 2^e and is rounded to nearest even;
  *                     a value that is not finite is stored as NaN and does not count in the maximum.  Others: rounded to nearest even.
- *                     Tokens at or behind cu_dev[B] and rows outside the cache are left out; other rows stay as they were.  n_tokens < 2^26.
+ *                     Tokens at or behind cu_dev[B] and rows outside the cache are left out; other rows stay as they were.  n_tokens < 2^25.
  * wf_op_cache_read    the same rows back: out_dev [n_tokens, 2 * 64 * n_heads] (keys of all heads, then values) of dtype f32 or bf16, contiguous.
  *                     Tokens behind the last sequence keep what out_dev holds; those whose row lies outside the cache read as zero.
  * wf_op_cache_attention   out[r, h, :] = sum_k w_k v_k, w = softmax over the visible keys k of scale * q[r, h, :] . k.  Row r of q, cu_q_dev[s] <= r
@@ -516,8 +516,8 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *                     mask_dev (uint32 [n_q_rows, mask_words]) a key k >= mask_from_dev[s] (NULL: 0) is seen only if bit
  *                     (k - mask_from_dev[s]) of row r's words is set (bit 0 = lowest bit of word 0; keys behind the last bit are not seen):
  *                     the tokens of a drafted tree, or of beams that share one cache, see their ancestors.  A row that sees no key gives
- *                     zeros, and what keys hold that a row does not see (infinities, NaN) does not reach it.  Query head h reads key / value
- *                     head h / (n_heads / cache->n_heads).  q and out: dtype f32 or bf16, the cache's own or, over an F8 cache, either; strides
+ *                     zeros (a logit of -infinity weighs nothing either), and what keys hold that a row does not see (infinities, NaN) does not
+ *                     reach it.  Query head h reads key / value head h / (n_heads / cache->n_heads).  q and out: dtype f32 or bf16, the cache's own or, over an F8 cache, either; strides
  *                     ldq, ldo in elements; q_dev, out_dev and both strides in bytes are multiples of 16 bytes.  max_q and max_len bound the
  *                     queries and keys of a sequence: len_dev[s] counts as max_len where it is larger, and as what the cache has from
  *                     row_dev[s] on; rows of a sequence behind its first max_q, and rows behind the last sequence, are left as they were.

@@ -233,7 +233,7 @@ int check_tokens(const wf_cache *c, const int32_t *cu, const int32_t *row, int32
   if (dtype != WF_DTYPE_F32 && dtype != WF_DTYPE_BF16) return host::fail(WF_E_INVALID_ARG, "dtype = %d", dtype);
   if (B < 1) return host::fail(WF_E_INVALID_ARG, "B = %d, need B >= 1", B);
   if (n_tokens < 0) return host::fail(WF_E_INVALID_ARG, "n_tokens = %d", n_tokens);
-  if (n_tokens >= 1 << 26) return host::fail(WF_E_CAPACITY, "n_tokens = %d (supported: below 2^26 a call)", n_tokens);      // 64 threads each, fewer than 2^32
+  if (n_tokens >= 1 << 25) return host::fail(WF_E_CAPACITY, "n_tokens = %d (supported: below 2^25 a call)", n_tokens);      // 64 threads each, fewer than 2^32 in all
   if (n_tokens == 0) return WF_OK;
   if (!cu || !row) return host::fail(WF_E_INVALID_ARG, "cu_dev or row_dev is NULL");
   return host::check_cache_memory(c);

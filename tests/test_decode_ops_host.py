@@ -57,7 +57,7 @@ def test_write_and_read_arguments():
         assert _write(c, **bad) == _read(c, **bad) == wf.WF_E_INVALID_ARG, bad
     for bad in (dict(ld=255), dict(n=5, k=None), dict(n=5, v=None), dict(n=5, k=P + 8), dict(n=5, v=P + 2), dict(n=5, ld=260)):
         assert _write(c, **bad) == wf.WF_E_INVALID_ARG, bad
-    assert _write(c, n=1 << 26) == _read(c, n=1 << 26) == wf.WF_E_CAPACITY
+    assert _write(c, n=1 << 25) == _read(c, n=1 << 25) == wf.WF_E_CAPACITY
     assert _read(c, n=5, out=None) == _read(c, n=5, out=P + 4) == wf.WF_E_INVALID_ARG
 
 
