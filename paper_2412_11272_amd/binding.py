@@ -752,16 +752,16 @@ def _index(t, n: int, here: int, what: str):
 
 
 def _rows_2d(t, here: int, what: str):
-    """A matrix [rows, columns] whose rows are contiguous; a third dimension (heads, 64) is folded.  Returns (rows, columns, row stride)."""
+    """A matrix [rows, columns] whose rows are contiguous, or [rows, heads, 64], whose heads are folded.  Returns (rows, columns, row stride)."""
     shape, stride = t.shape, t.stride()
     if t.get_device() != here:
         raise ValueError(f"{what} is on {t.device}, need the current CUDA device")
     if len(shape) == 2 and (stride[1] == 1 or shape[1] == 1):
         n, cols = shape
-    elif len(shape) == 3 and stride[2] == 1 and (stride[1] == shape[2] or shape[1] <= 1):
-        n, cols = shape[0], shape[1] * shape[2]
+    elif len(shape) == 3 and shape[2] == 64 and stride[2] == 1 and (stride[1] == 64 or shape[1] <= 1):
+        n, cols = shape[0], shape[1] * 64
     else:
-        raise ValueError(f"{what}: shape {tuple(shape)}, strides {stride}: need rows of contiguous values")
+        raise ValueError(f"{what}: shape {tuple(shape)}, strides {stride}: need rows of contiguous values, [n, 64 n_heads] or [n, n_heads, 64]")
     return n, cols, stride[0] if n > 1 else cols
 
 

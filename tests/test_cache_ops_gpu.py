@@ -501,3 +501,17 @@ def test_calls_on_two_streams_at_once():
     for i in range(2):
         for g in got[i]:
             assert torch.equal(g, want[i])
+
+
+@pytest.mark.parametrize("heads", [(4, 128), (16, 32)], ids=str)
+def test_heads_of_another_size_are_refused(heads):
+    cache = _filled(20, 8, BF, 60)
+    args = (_i32([0, 3]), _i32([0]))
+    x, other = _q(3, 8, BF, 61), _q(3, 8, BF, 62).view(3, *heads)
+    for k, v in ((other, other), (x, other), (other, x)):
+        with pytest.raises(ValueError):
+            wf.op_cache_write(cache, k, v, *args)
+    with pytest.raises(ValueError):
+        wf.op_cache_attention(cache, other, *args, _i32([20]), 3, 20)
+    with pytest.raises(ValueError):
+        wf.op_cache_attention(cache, x, *args, _i32([20]), 3, 20, out=torch.empty_like(other))

@@ -140,6 +140,23 @@ def test_binding_refuses_host_tensors():
         wf.op_beam_reorder(torch.zeros((1, 2, 3)), torch.zeros((1, 2), dtype=torch.int32))
 
 
+@pytest.mark.parametrize("shape", [(5, 4, 32), (5, 4, 128), (5, 1, 128), (0, 2, 32), (5, 2, 64, 1)], ids=str)
+def test_a_third_dimension_is_a_heads_64_values(shape):
+    """[n, 4, 128] is no 8 heads of 64: folding it would cut its heads in two."""
+    with pytest.raises(ValueError, match="q"):
+        wf._rows_2d(torch.zeros(shape), -1, "q")
+
+
+def test_rows_of_heads_and_their_strides():
+    wide = torch.zeros((7, 6, 64))
+    assert wf._rows_2d(wide, -1, "q") == wf._rows_2d(wide.view(7, 384), -1, "q") == (7, 384, 384)
+    assert wf._rows_2d(wide[:, 2:4], -1, "q") == (7, 128, 384)
+    assert wf._rows_2d(wide[:, 3:4], -1, "q") == (7, 64, 384) and wf._rows_2d(wide[:1, 2:4], -1, "q") == (1, 128, 128)
+    for bad in (wide[:, ::2], wide[:, :, ::2], wide.transpose(1, 2), wide.view(7, 384).t()):
+        with pytest.raises(ValueError):
+            wf._rows_2d(bad, -1, "q")
+
+
 # ---- the oracle's own pins ------------------------------------------------------------------------------------------------
 def test_oracle_format_is_torchs_e4m3():
     codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
