@@ -498,7 +498,7 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *   WF_DTYPE_F32, WF_DTYPE_BF16   data_dev [n_rows, 2 * 64 * n_heads]: the keys of all heads, then the values (a layer of wf_cross_kv's or
  *                 wf_prefill's buffers is such a cache as it stands); exps_dev is NULL;
  *   WF_DTYPE_F8   data_dev [n_rows, n_heads, 2, 64] e4m3 (OCP, no infinity): of each head 64 key values, then 64 values; exps_dev uint8
- *                 [2 * n_heads, n_rows]: entry (2 h, r) for the keys, (2 h + 1, r) for the values of head h in row r.  A stored q stands for
+ *                 [2 * n_heads, n_rows]: entry (2 h, r) for the keys, (2 h + 1, r) for the values of head h in row r, 0 .. 254.  A stored q stands for
  *                 q * 2^(exponent - 127).
  * data_dev is aligned to 16 bytes.  A sequence is a range of consecutive rows.  Ranges may overlap where they are read; what rows hold that two
  * sequences of one call write is not defined.
@@ -507,7 +507,8 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *                     row_dev[s] + t - cu_dev[s] (DEVICE int32 [B]).  k_dev, v_dev: [n_tokens, 64 * n_heads] of dtype f32 or bf16, row stride
  *                     ld elements (>= 64 * n_heads; both pointers and ld * element size multiples of 16 bytes).  F8: each head's key and
  *                     value vector gets the smallest power of two 2^e >= 2^-127 with max|x| <= 448 * 2^e and is rounded to nearest even;
- *                     a value that is not finite is stored as NaN and does not count in the maximum.  Others: rounded to nearest even.
+ *                     a value that is not finite is stored as NaN and does not count in the maximum; finite values stay finite: those of 1.875 * 2^127
+ *                     and more in magnitude are stored as that value (the next code would stand for 2^128).  Others: rounded to nearest even.
  *                     Tokens at or behind cu_dev[B] and rows outside the cache are left out; other rows stay as they were.  n_tokens < 2^25.
  * wf_op_cache_read    the same rows back: out_dev [n_tokens, 2 * 64 * n_heads] (keys of all heads, then values) of dtype f32 or bf16, contiguous.
  *                     Tokens behind the last sequence keep what out_dev holds; those whose row lies outside the cache read as zero.

@@ -18,8 +18,8 @@ def e4m3_values() -> np.ndarray:
 
 
 def quantise(x: np.ndarray):
-    """x [.., 64] -> (values q [.., 64], biased exponents [..]): e = the smallest whole number >= -127 with max|x| <= 448 2^e over the finite
-    x, q = x 2^-e rounded to e4m3, ties to the even code; NaN where x is not finite."""
+    """x [.., 64] of fp32's range -> (values q [.., 64], biased exponents [..]): e = the smallest whole number >= -127 with max|x| <= 448 2^e over
+    the finite x, q = x 2^-e rounded to e4m3, ties to the even code, but to 240 where 2^128 would be nearest; NaN where x is not finite."""
     x = np.asarray(x, np.float64)
     fine = np.isfinite(x)
     largest = np.where(fine, np.abs(x), 0.0).max(-1)
@@ -35,7 +35,8 @@ def quantise(x: np.ndarray):
     up, down = mag[hi] - a, a - mag[lo]
     code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)
     code = np.where(mag[hi] == a, hi, code)
-    q = np.where(fine, np.copysign(mag[code], y), np.nan)
+    most = np.where(e[..., None] >= 120, 240.0, 448.0)         # q 2^e below 2^128
+    q = np.where(fine, np.copysign(np.minimum(mag[code], most), y), np.nan)
     return q, e + 127
 
 

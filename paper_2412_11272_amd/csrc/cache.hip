@@ -2,8 +2,9 @@
 // rules are stated with the declarations in include/wf_encoder.h.
 //
 // Quantisation of a head's 64 values x: e = min{whole e >= -127 : max|x| <= 448 2^e}, q = round(x 2^-e) in e4m3.  A power of two keeps
-// the product x 2^-e exact, so that q has one rounding (to nearest even, half a step of 2^-4 relative to the value) and a reader gets
-// q 2^e exactly in bf16 or fp32.
+// the product x 2^-e exact, so that q has one rounding (to nearest even, half a step of 2^-4 relative to the value).  A reader gets q 2^e
+// exactly in fp32, and in bf16 from e = -124 on (q's smallest step is 2^-9, bf16's 2^-133; below, a bf16 reader rounds once more).  At the other end
+// 256 * 2^120 would be 2^128: kMostF8 = 240 * 2^120 is the largest value that a code and an exponent stand for, and finite values end there.
 #include "cache_device.h"
 #include "host_runtime.h"
 
@@ -93,6 +94,8 @@ __device__ __forceinline__ float max_of_8_lanes(float v) {
   return fmaxf(v, dpp<0x141>(v));
 }
 
+constexpr float kMostF8 = 0x1.ep127f;
+
 template <int CACHE> struct Stored { typedef __bf16 type; };
 template <> struct Stored<WF_DTYPE_F32> { typedef float type; };
 
@@ -125,7 +128,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheView c, const T *
         for (int e = 0; e < 8; ++e) {
           const bool fine = (__builtin_bit_cast(uint32_t, f[e]) & 0x7f800000u) != 0x7f800000u;
           largest = fmaxf(largest, fine ? fabsf(f[e]) : 0.0f);
-          f[e] = fine ? f[e] : __builtin_nanf("");
+          f[e] = fine ? __builtin_amdgcn_fmed3f(f[e], -kMostF8, kMostF8) : __builtin_nanf("");
         }
         const uint32_t biased = f8_exponent(max_of_8_lanes(largest));
         const float factor = __builtin_bit_cast(float, (254u - biased) << 23);

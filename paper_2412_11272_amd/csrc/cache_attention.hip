@@ -21,7 +21,7 @@
 //
 // Rounding: logits, statistics and sums are fp32.  Next to bf16 the weights enter as the sum of two bf16 parts (2^-17 of a weight is lost, where
 // one part would lose 2^-9): twice the second product's instructions, of which the kernel has plenty to spare.  Values of the 8-bit caches with their
-// powers of two are exact in either operand type.
+// powers of two are exact as fp32 operands, and as bf16 operands from 2^-124 on.
 #include "cache_device.h"
 #include "host_runtime.h"
 

@@ -515,3 +515,26 @@ def test_heads_of_another_size_are_refused(heads):
         wf.op_cache_attention(cache, other, *args, _i32([20]), 3, 20)
     with pytest.raises(ValueError):
         wf.op_cache_attention(cache, x, *args, _i32([20]), 3, 20, out=torch.empty_like(other))
+
+
+@pytest.mark.parametrize("src", [BF, F32], ids=str)
+def test_finite_values_come_back_finite(src):
+    # next to the largest finite value the nearest code would stand for 2^128
+    top = torch.finfo(src).max
+    x = torch.zeros((3, 64))
+    x[0, :3] = torch.tensor([top, -top, 1.5 * 2.0 ** 127])
+    x[1, :4] = torch.tensor([1.9375 * 2.0 ** 127, 1.875 * 2.0 ** 127, 1.75 * 2.0 ** 127, -1.0])
+    x[2] = -top
+    x = x.to(src)
+    cache = wf.Cache.empty(3, 1, F8)
+    wf.op_cache_write(cache, x.cuda(), x.cuda(), _i32([0, 3]), _i32([0]))
+    q, e = D.quantise(x.double().numpy())
+    want = q * 2.0 ** (e[:, None] - 127.0)
+    assert np.isfinite(want.astype(np.float32)).all()
+    for out_dtype in (F32, BF):
+        back = wf.op_cache_read(cache, _i32([0, 3]), _i32([0]), 3, out_dtype=out_dtype)
+        np.testing.assert_array_equal(_np(back).reshape(3, 2, 64), np.stack([want, want], 1))       # e4m3's 4 bits fit both types
+    # one key has all the weight: its value comes out as it is
+    for act in (BF, F32):
+        out = wf.op_cache_attention(cache, torch.zeros((3, 64), dtype=act, device="cuda"), _i32([0, 1, 2, 3]), _i32([0, 1, 2]), _i32([1, 1, 1]), 1, 1)
+        np.testing.assert_array_equal(_np(out), want)

@@ -172,6 +172,19 @@ def test_oracle_format_is_torchs_e4m3():
     assert b.tolist() == [0, 119, 0] and not q[0].any() and np.isnan(q[1, :3]).all() and q[1, 3] == 256.0 and not q[2].any()
 
 
+def test_oracle_keeps_finite_values_finite():
+    top = float(np.finfo(np.float32).max)
+    x = np.zeros((4, 64))
+    x[0, :3] = top, -top, 1.5 * 2.0 ** 127
+    x[1, :2] = 1.9375 * 2.0 ** 127, 1.9374 * 2.0 ** 127            # where rounding would go up to 2^128, and just below
+    x[2, :2] = 1.75 * 2.0 ** 127, 1.0                              # one exponent lower: 448 itself is a finite value there
+    x[3] = top
+    q, b = D.quantise(x)
+    assert b.tolist() == [247, 247, 246, 247]
+    assert q[0, :3].tolist() == [240.0, -240.0, 192.0] and q[1, :2].tolist() == [240.0, 240.0] and q[2, 0] == 448.0 and (q[3] == 240.0).all()
+    assert (np.abs(q) * 2.0 ** (b[:, None] - 127.0) <= top).all()
+
+
 def test_oracle_attention_is_a_softmax_over_the_visible_keys():
     rng = np.random.default_rng(0)
     q, k, v = rng.standard_normal(64), rng.standard_normal((40, 64)), rng.standard_normal((40, 64))
