@@ -55,6 +55,10 @@ struct AttendArgs {
   float scale;
 };
 
+// Ranges of split_keys keys that n >= 1 keys take; n + split_keys may pass 2^31.
+__host__ __device__ constexpr int ranges_of(int n, int split_keys) { return (n - 1) / split_keys + 1; }
+static_assert(ranges_of(1, kTile) == 1 && ranges_of(kTile + 1, kTile) == 2 && ranges_of((1 << 30) + 1, 1 << 30) == 2 && ranges_of(INT32_MAX, 1 << 30) == 2, "");
+
 // The keys of sequence s: their number and the first row.
 __device__ __forceinline__ int sequence_keys(const AttendArgs &p, int s, int64_t *row0) {
   *row0 = p.row[s];
@@ -590,7 +594,7 @@ __global__ void __launch_bounds__(256) cache_attention_join_kernel(AttendArgs p,
   int64_t row0;
   const int n = sequence_keys(p, s, &row0);
   if (n <= p.split_keys) return;
-  const int parts = (n + p.split_keys - 1) / p.split_keys;
+  const int parts = ranges_of(n, p.split_keys);
   static_assert(kMaxSplits <= 64, "a lane per part");
   const f32x2 ml = lane < parts ? *(const f32x2 *)(p.part_ml + 2 * (unit * p.n_split + lane)) : f32x2{-INFINITY, 0.0f};
   const float m_one = ml[0], l_one = ml[1];

@@ -538,3 +538,23 @@ def test_finite_values_come_back_finite(src):
     for act in (BF, F32):
         out = wf.op_cache_attention(cache, torch.zeros((3, 64), dtype=act, device="cuda"), _i32([0, 1, 2, 3]), _i32([0, 1, 2]), _i32([1, 1, 1]), 1, 1)
         np.testing.assert_array_equal(_np(out), want)
+
+
+def test_a_split_sequence_next_to_the_largest_length():
+    # Bounds of 2^31 - 1 keys split in two: a sequence just longer than a part, whose last keys alone hold something.  Keys of zero weigh the same.
+    n, B = (1 << 30) + 70, 512
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("needs 140 GB for one cache")
+    data = torch.zeros((n, 1, 2, 64), dtype=torch.uint8, device="cuda")
+    exps = torch.full((2, n), 127, dtype=torch.uint8, device="cuda")
+    data[1 << 30:, 0, 1] = 0x38                        # 1
+    exps[1, 1 << 30:] = 127 + 30
+    cache = wf.Cache(data.view(F8), exps)
+    lens = [5] * B
+    lens[77] = n
+    out = wf.op_cache_attention(cache, _q(B, 1, BF, 63), _i32(range(B + 1)), _i32([0] * B), _i32(lens), 1, 2 ** 31 - 1)
+    got, want = _np(out), 70 * 2.0 ** 30 / n
+    assert (np.abs(got[77] - want) <= 2.0 ** -8 * want).all()         # sums of whole numbers below 2^24 of them and their multiples: exact
+    assert not got[:77].any() and not got[78:].any()
+    del cache, data, exps
+    torch.cuda.empty_cache()
