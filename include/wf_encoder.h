@@ -518,7 +518,8 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *                     (k - mask_from_dev[s]) of row r's words is set (bit 0 = lowest bit of word 0; keys behind the last bit are not seen):
  *                     the tokens of a drafted tree, or of beams that share one cache, see their ancestors.  A row that sees no key gives
  *                     zeros (a logit of -infinity weighs nothing either), and what keys hold that a row does not see (infinities, NaN) does not
- *                     reach it.  Query head h reads key / value head h / (n_heads / cache->n_heads).  q and out: dtype f32 or bf16, the cache's own or, over an F8 cache, either; strides
+ *                     reach it.  Logits and sums are fp32: a row that sees a logit of 2^127 or more may give NaN, one of values beyond 2^119 / len
+ *                     infinity.  Query head h reads key / value head h / (n_heads / cache->n_heads).  q and out: dtype f32 or bf16, the cache's own or, over an F8 cache, either; strides
  *                     ldq, ldo in elements; q_dev, out_dev and both strides in bytes are multiples of 16 bytes.  max_q and max_len bound the
  *                     queries and keys of a sequence: len_dev[s] counts as max_len where it is larger, and as what the cache has from
  *                     row_dev[s] on; rows of a sequence behind its first max_q, and rows behind the last sequence, are left as they were.
@@ -568,7 +569,7 @@ typedef struct {
   int32_t n_heads;              /* query heads, a multiple of the cache's */
   int32_t n_seqs, n_q_rows, max_q, max_len;
   int32_t mask_words;
-  float scale;                  /* finite */
+  float scale;                  /* finite, and so is log2(e) * scale */
 } wf_cache_query;
 
 typedef struct {

@@ -423,7 +423,8 @@ __global__ void __launch_bounds__(64 * NW, NQ == 1 && sizeof(T) == 2 ? 3 : 2) ca
         for (int j = 1; j < 8; ++j) top = fmaxf(top, x[k][j]);
         rise |= (top > -INFINITY) & (top * c > st[t].m + 8.0f);
       }
-      // A row's reference follows its maximum only where that is 2^8 above it: weights of up to 2^8 lose nothing in fp32.
+      // A row's reference follows its maximum only where that is 2^8 above it: weights of up to 2^8 lose nothing in fp32.  The reference stays
+      // finite: against one of infinity even the largest logit's weight would be 0, and a row of logits beyond fp32 would look like one that sees nothing.
       if (__ballot(rise)) {
 #pragma unroll
         for (int k = 0; k < GT; ++k) {
@@ -433,7 +434,7 @@ __global__ void __launch_bounds__(64 * NW, NQ == 1 && sizeof(T) == 2 ? 3 : 2) ca
           for (int j = 1; j < 8; ++j) top = fmaxf(top, x[k][j]);
           const Pair rp = row_pair(top);
           top = half_max(fmaxf(rp.a, rp.b));
-          top = top == -INFINITY ? w.m : fmaxf(w.m, top * c);
+          top = top == -INFINITY ? w.m : fmaxf(w.m, fminf(top * c, 3.4028234664e38f));
           const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - top);
           w.l *= keep;
 #pragma unroll
@@ -689,7 +690,7 @@ int check_query(const wf_cache *c, const wf_cache_query *a) {
     return fail(WF_E_INVALID_ARG, "n_heads = %d must be a multiple of the cache's %d", a->n_heads, c->n_heads);
   if (a->n_seqs < 1 || a->n_q_rows < 0 || a->max_q < 1 || a->max_len < 0)
     return fail(WF_E_INVALID_ARG, "n_seqs = %d, n_q_rows = %d, max_q = %d, max_len = %d", a->n_seqs, a->n_q_rows, a->max_q, a->max_len);
-  if (!std::isfinite(a->scale)) return fail(WF_E_INVALID_ARG, "scale is not finite");
+  if (!std::isfinite(a->scale * 1.4426950408889634f)) return fail(WF_E_INVALID_ARG, "scale = %g: it and log2(e) times it must be finite", a->scale);
   if ((double)a->n_seqs * std::min(a->max_q, std::max(a->n_q_rows, 1)) * a->n_heads >= (double)(1 << 30) || (double)a->n_seqs * c->n_heads >= (double)(1 << 24))
     return fail(WF_E_CAPACITY, "%d sequences of up to %d queries of %d heads: more than 2^30 rows or 2^24 heads", a->n_seqs, a->max_q, a->n_heads);
   return WF_OK;

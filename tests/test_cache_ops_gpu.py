@@ -558,3 +558,23 @@ def test_a_split_sequence_next_to_the_largest_length():
     assert not got[:77].any() and not got[78:].any()
     del cache, data, exps
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n_keys", [40, 1600])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("act,cdtype", KINDS)
+def test_logits_beyond_fp32_do_not_look_like_no_keys(act, cdtype, masked, n_keys):
+    # q . k = 64 * 2^63 is finite, 2^60 times it is not: NaN and no zeros; rows of ordinary logits beside them stay as they are
+    cache = wf.Cache.empty(n_keys, 1, cdtype)
+    x = torch.zeros((n_keys, 64), dtype=act if cdtype == F8 else cdtype, device="cuda")
+    x[:, :] = 2.0 ** 63
+    wf.op_cache_write(cache, x, torch.ones_like(x), _i32([0, n_keys]), _i32([0]))
+    q = torch.zeros((18, 64), dtype=act, device="cuda")
+    q[1], q[17] = 1.0, 1.0
+    q[2] = -1.0                                        # every logit -infinity in fp32: each weighs nothing
+    mask = torch.full((18, 2), -1, dtype=torch.int32, device="cuda") if masked else None
+    for n_q in (3, 18):
+        out = _np(wf.op_cache_attention(cache, q[:n_q], _i32([0, n_q]), _i32([0]), _i32([n_keys]), n_q, n_keys, scale=2.0 ** 60,
+                                        mask=mask if mask is None else mask[:n_q]))
+        assert np.isnan(out[1]).all() and (out[0] == 1.0).all() and not out[2].any() and (out[3:17] == 1.0).all()
+        assert n_q == 3 or np.isnan(out[17]).all()

@@ -91,6 +91,13 @@ def test_attention_arguments():
     assert call(n_q_rows=2, max_len=1 << 20, workspace_dev=P + 8, workspace_bytes=need) == wf.WF_E_INVALID_ARG
 
 
+def test_a_scale_whose_binary_logits_overflow():
+    c = _cache()
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        assert wf.lib().wf_op_cache_attention(C.byref(c), C.byref(_query(scale=scale)), None) == wf.WF_E_INVALID_ARG
+    assert wf.lib().wf_op_cache_attention(C.byref(c), C.byref(_query(scale=-2.3e38)), None) == wf.WF_OK
+
+
 def _step(**kw):
     return wf.WfBeamStep(**{**dict(logits_dev=P, ld=100, score_in_dev=P, token_out_dev=P, parent_out_dev=P, score_out_dev=P, workspace_dev=P,
                                    workspace_bytes=0, dtype=wf.WF_DTYPE_F32, B=2, width=5, n_vocab=100, eos=-1), **kw})
