@@ -727,16 +727,18 @@ def _here(t, what: str) -> int:
     """The device of a tensor, which has to be the current one: a launch goes to the current device's stream."""
     import torch
     d = t.get_device()
-    if d < 0 or d != torch._C._cuda_getDevice():
+    if d < 0 or d != torch.cuda.current_device():
         raise ValueError(f"{what} is on {t.device}, need the current CUDA device")
     return d
 
 
 def _stream_on(stream, here: int) -> int:
+    """_raw_stream, the current device being known."""
     if stream is not None:
         return stream
     import torch
-    return torch._C._cuda_getCurrentRawStream(here)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(here) if raw else torch.cuda.current_stream().cuda_stream
 
 
 def _index(t, n: int, here: int, what: str):

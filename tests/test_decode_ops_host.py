@@ -1,6 +1,7 @@
 """CPU-only checks of the decoding operators' entry points: what the host refuses before it launches anything, what it
 accepts without work to do, and the oracle's own pins."""
 import ctypes as C
+import types
 
 import numpy as np
 import pytest
@@ -145,6 +146,21 @@ def test_binding_refuses_host_tensors():
         wf.op_beam_select(torch.zeros((1, 2, 10)), torch.zeros((1, 2)))
     with pytest.raises(ValueError):
         wf.op_beam_reorder(torch.zeros((1, 2, 3)), torch.zeros((1, 2), dtype=torch.int32))
+
+
+def test_device_and_stream_of_a_call_without_torchs_private_functions(monkeypatch):
+    """torch's private handles are used where this torch has them and not relied on."""
+    t = types.SimpleNamespace(get_device=lambda: 3, device="cuda:3")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=55))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
+    assert wf._here(t, "q") == 3 and wf._stream_on(None, 3) == 103 and wf._stream_on(0, 3) == 0 and wf._stream_on(77, 3) == 77
+    for private in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.delattr(torch._C, private, raising=False)
+    assert wf._here(t, "q") == 3 and wf._stream_on(None, 3) == 55
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 2)
+    with pytest.raises(ValueError, match="q is on cuda:3"):
+        wf._here(t, "q")
 
 
 @pytest.mark.parametrize("shape", [(5, 4, 32), (5, 4, 128), (5, 1, 128), (0, 2, 32), (5, 2, 64, 1)], ids=str)
