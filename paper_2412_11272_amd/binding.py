@@ -5,6 +5,7 @@ There is no fallback: if the shared library is missing, loading raises."""
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from typing import List, Optional, Sequence, Tuple
 
@@ -723,11 +724,16 @@ def op_ln_linear(x, g, b, w, bias, out, epilogue: int, eps: float = 1e-5, stream
 
 # ---- token-by-token decoding: caches, attention over them, beams -------------------------------
 # (Called once per layer and token: a check is an attribute or two, and nothing is built that a launch does not need.)
+def _current_device(torch):
+    """What tells the current device (torch's own handle where this torch gives it away)."""
+    return getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _here(t, what: str) -> int:
     """The device of a tensor, which has to be the current one: a launch goes to the current device's stream."""
     import torch
     d = t.get_device()
-    if d < 0 or d != torch.cuda.current_device():
+    if d < 0 or d != _current_device(torch)():
         raise ValueError(f"{what} is on {t.device}, need the current CUDA device")
     return d
 
@@ -798,24 +804,36 @@ def _fill_workspace(a, need: int, workspace, like, here: int, stream):
 
 class Cache:
     """Keys and values of heads of size 64 on the device (wf_cache): `data` [n_rows, 128 n_heads] float32 or bfloat16 (keys of all heads, then
-    values: a layer of what Decoder.cross_kv or prefill returns), or [n_rows, n_heads, 2, 64] float8_e4m3fn with `exps` uint8 [2 n_heads, n_rows]."""
+    values: a layer of what Decoder.cross_kv or prefill returns), or [n_rows, n_heads, 2, 64] float8_e4m3fn with `exps` uint8 [2 n_heads, n_rows].
+    It stands for the memory it was made of: its tensors' contents may change, other or moved tensors need a new Cache."""
+    data, exps, n_rows, n_heads, device = (property(operator.attrgetter(name)) for name in ("_data", "_exps", "_n_rows", "_n_heads", "_device"))
 
     def __init__(self, data, exps=None):
         import torch
         shape = data.shape
         f8 = data.dtype == torch.float8_e4m3fn
-        self.device = data.get_device()          # a call checks that it is the current one
-        if self.device < 0:
+        self._device = data.get_device()         # a call checks that it is the current one
+        if self._device < 0:
             raise ValueError(f"data is on {data.device}, need a CUDA device")
         if not data.is_contiguous() or (len(shape) != 4 or shape[2] != 2 or shape[3] != 64 if f8 else len(shape) != 2 or shape[1] % 128):
             raise ValueError(f"data: {tuple(shape)} with strides {data.stride()}, need [n_rows, 128 n_heads] or, in 8 bits, [n_rows, n_heads, 2, 64]")
         n_rows, n_heads = shape[0], shape[1] if f8 else shape[1] // 128
         if f8 != (exps is not None):
             raise ValueError("exps goes with float8_e4m3fn data and with no other")
-        if f8 and (exps.dtype != torch.uint8 or exps.get_device() != self.device or exps.shape != (2 * n_heads, n_rows) or not exps.is_contiguous()):
+        if f8 and (exps.dtype != torch.uint8 or exps.get_device() != self._device or exps.shape != (2 * n_heads, n_rows) or not exps.is_contiguous()):
             raise ValueError(f"exps: {tuple(exps.shape)} {exps.dtype} on {exps.device}, need uint8 [{2 * n_heads}, {n_rows}] beside the data")
-        self.data, self.exps, self.n_rows, self.n_heads = data, exps, n_rows, n_heads
-        self._c = WfCache(data.data_ptr(), exps.data_ptr() if f8 else None, n_rows, n_heads, WF_DTYPE_F8 if f8 else _torch_dtype_code(data.dtype))
+        self._data, self._exps, self._n_rows, self._n_heads = data, exps, n_rows, n_heads
+        self._data_at, self._exps_at = data.data_ptr(), exps.data_ptr() if f8 else None
+        self._current = _current_device(torch)
+        self._c = WfCache(self._data_at, self._exps_at, n_rows, n_heads, WF_DTYPE_F8 if f8 else _torch_dtype_code(data.dtype))
+
+    def _here(self) -> int:
+        """The current device, which has to be the cache's; its memory has to be where it was."""
+        if self._data.data_ptr() != self._data_at or (self._exps is not None and self._exps.data_ptr() != self._exps_at):
+            raise ValueError("the cache's tensors have moved: make a new Cache of them")
+        if self._current() != self._device:
+            raise ValueError(f"cache is on {self._data.device}, need the current CUDA device")
+        return self._device
 
     @classmethod
     def empty(cls, n_rows: int, n_heads: int, dtype, device="cuda") -> "Cache":
@@ -830,9 +848,9 @@ class Cache:
 def op_cache_write(cache: Cache, k, v, cu, rows, stream=None) -> Cache:
     """Token t of sequence s (cu[s] <= t < cu[s + 1]) into cache row rows[s] + t - cu[s].  k, v: [n_tokens, 64 n_heads] or [n_tokens, n_heads,
     64], views into wider rows (a projection's output) with one row stride; cu [B + 1], rows [B]: int32 on the device."""
-    here = _here(cache.data, "cache")
+    here = cache._here()
     n, cols, ld = _rows_2d(k, here, "k")
-    if _rows_2d(v, here, "v") != (n, cols, ld) or v.dtype != k.dtype or cols != 64 * cache.n_heads:
+    if _rows_2d(v, here, "v") != (n, cols, ld) or v.dtype != k.dtype or cols != 64 * cache._n_heads:
         raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}: need two [n_tokens, {64 * cache.n_heads}] of one type and row stride")
     B = rows.numel()
     _check(lib().wf_op_cache_write(C.byref(cache._c), k.data_ptr(), v.data_ptr(), _torch_dtype_code(k.dtype), ld, _index(cu, B + 1, here, "cu"),
@@ -843,9 +861,9 @@ def op_cache_write(cache: Cache, k, v, cu, rows, stream=None) -> Cache:
 def op_cache_read(cache: Cache, cu, rows, n_tokens: int, out=None, out_dtype=None, stream=None):
     """The rows op_cache_write fills, as [n_tokens, 128 n_heads] (keys of all heads, then values)."""
     import torch
-    here = _here(cache.data, "cache")
+    here = cache._here()
     if out is None:
-        out = _empty((n_tokens, 128 * cache.n_heads), out_dtype or torch.bfloat16, cache.data, stream)
+        out = _empty((n_tokens, 128 * cache._n_heads), out_dtype or torch.bfloat16, cache._data, stream)
     elif out.shape != (n_tokens, 128 * cache.n_heads) or not out.is_contiguous() or out.get_device() != here:
         raise ValueError(f"out: {tuple(out.shape)} on {out.device}, need a contiguous [{n_tokens}, {128 * cache.n_heads}] beside the cache")
     B = rows.numel()
@@ -860,7 +878,7 @@ def op_cache_attention(cache: Cache, q, cu_q, rows, lens, max_q: int, max_len: i
     [n_q_rows, n_heads, 64]; cu_q [B + 1], rows, lens [B]: int32 on the device; max_q, max_len: upper bounds of a sequence's queries and keys.
     mask: int32 [n_q_rows, words], bit k - mask_from[s] (mask_from: int32 [B], None: 0) says whether a row sees key k; keys before
     mask_from[s] are seen by all."""
-    here = _here(cache.data, "cache")
+    here = cache._here()
     n, cols, ldq = _rows_2d(q, here, "q")
     if cols % 64:
         raise ValueError(f"q: {cols} columns, need 64 for each head")

@@ -578,3 +578,17 @@ def test_logits_beyond_fp32_do_not_look_like_no_keys(act, cdtype, masked, n_keys
                                         mask=mask if mask is None else mask[:n_q]))
         assert np.isnan(out[1]).all() and (out[0] == 1.0).all() and not out[2].any() and (out[3:17] == 1.0).all()
         assert n_q == 3 or np.isnan(out[17]).all()
+
+
+def test_calls_do_not_follow_a_cache_whose_memory_moved():
+    for dtype in (BF, F8):
+        cache = _filled(40, 2, dtype, 64)
+        q, args = _q(2, 2, BF, 65), (_i32([0, 2]), _i32([0]))
+        with pytest.raises(AttributeError):
+            cache.data = torch.zeros_like(cache.data)
+        t = cache.data if dtype == BF else cache.exps
+        t.resize_(400 * t.shape[0], *t.shape[1:])
+        for call in (lambda: wf.op_cache_write(cache, q, q, *args), lambda: wf.op_cache_read(cache, *args, 2),
+                     lambda: wf.op_cache_attention(cache, q, *args, _i32([9]), 2, 9)):
+            with pytest.raises(ValueError):
+                call()

@@ -154,9 +154,10 @@ def test_device_and_stream_of_a_call_without_torchs_private_functions(monkeypatc
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=55))
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 3, raising=False)
     assert wf._here(t, "q") == 3 and wf._stream_on(None, 3) == 103 and wf._stream_on(0, 3) == 0 and wf._stream_on(77, 3) == 77
     for private in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
-        monkeypatch.delattr(torch._C, private, raising=False)
+        monkeypatch.delattr(torch._C, private)
     assert wf._here(t, "q") == 3 and wf._stream_on(None, 3) == 55
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 2)
     with pytest.raises(ValueError, match="q is on cuda:3"):
@@ -178,6 +179,33 @@ def test_rows_of_heads_and_their_strides():
     for bad in (wide[:, ::2], wide[:, :, ::2], wide.transpose(1, 2), wide.view(7, 384).t()):
         with pytest.raises(ValueError):
             wf._rows_2d(bad, -1, "q")
+
+
+def _fake(shape, dtype, at, device=0):
+    """What Cache asks of a tensor on a device."""
+    t = torch.empty(shape, dtype=dtype, device="meta")
+    return types.SimpleNamespace(shape=t.shape, dtype=dtype, device=f"cuda:{device}", get_device=lambda: device, is_contiguous=lambda: True, stride=t.stride,
+                                 data_ptr=lambda: at)
+
+
+def test_a_cache_keeps_to_the_memory_it_was_made_of(monkeypatch):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    data, exps = _fake((9, 2, 2, 64), torch.float8_e4m3fn, 4096), _fake((4, 9), torch.uint8, 1 << 20)
+    c = wf.Cache(data, exps)
+    assert (c.data, c.exps, c.n_rows, c.n_heads, c.device) == (data, exps, 9, 2, 0) and c._here() == 0
+    assert (c._c.data_dev, c._c.exps_dev) == (4096, 1 << 20)
+    for name in ("data", "exps", "n_rows", "n_heads", "device"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, getattr(c, name))
+    for t in (data, exps):                                          # grown in place, its memory is elsewhere
+        was, t.data_ptr = t.data_ptr, lambda: 1 << 30
+        with pytest.raises(ValueError, match="moved"):
+            c._here()
+        t.data_ptr = was
+    assert c._here() == 0
+    c = wf.Cache(_fake((9, 256), torch.bfloat16, 4096, device=1))
+    with pytest.raises(ValueError, match="cuda:1"):
+        c._here()
 
 
 # ---- the oracle's own pins ------------------------------------------------------------------------------------------------
