@@ -435,7 +435,7 @@ int wf_op_beam_reorder(void *dst_dev, const void *src_dev, const int32_t *parent
   const uintptr_t d = (uintptr_t)dst_dev, f = (uintptr_t)src_dev;
   if (d != f && d < f + (uintptr_t)all && f < d + (uintptr_t)all) return fail(WF_E_INVALID_ARG, "dst_dev and src_dev overlap");
   const int vec = (d | f | (uintptr_t)slot | (uintptr_t)pos_bytes) % 16 == 0 ? 16 : (d | f | (uintptr_t)slot | (uintptr_t)pos_bytes) % 4 == 0 ? 4 : 1;
-  ReorderArgs p{dst_dev, src_dev, parent_dev, len_dev, B, width, n_pos, pos_bytes, slot, (slot + 256 * vec - 1) / (256 * vec)};      // the most workgroups of any form
+  ReorderArgs p{dst_dev, src_dev, parent_dev, len_dev, B, width, n_pos, pos_bytes, slot, (slot - 1) / (256 * vec) + 1};      // the most workgroups of any form
   if ((int64_t)n_layers * B * (double)p.chunks >= (double)(1 << 24))
     return fail(WF_E_CAPACITY, "%lld bytes in %d layers, moved %d at a time: more than 2^32 threads", (long long)all, n_layers, vec);
   const int64_t ls = (int64_t)n_layers * B;

@@ -139,6 +139,12 @@ def test_beam_reorder_arguments():
     assert _step_over(n_vocab=(1 << 28) + 1) == wf.WF_E_CAPACITY
 
 
+@pytest.mark.parametrize("n_pos,pos_bytes", [((1 << 63) - 1, 1), ((1 << 63) - 4096, 1), (1, (1 << 63) - 16), ((1 << 62) - 1, 2)], ids=str)
+def test_slots_next_to_the_largest_number_of_bytes(n_pos, pos_bytes):
+    """Rounding such a slot up to whole workgroups leaves 64 bits."""
+    assert wf.lib().wf_op_beam_reorder(P, P, P, None, 1, 1, 1, n_pos, pos_bytes, None) == wf.WF_E_CAPACITY
+
+
 def test_binding_refuses_host_tensors():
     with pytest.raises(ValueError):
         wf.Cache(torch.zeros((4, 128)))
