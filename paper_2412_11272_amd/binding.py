@@ -747,6 +747,11 @@ def _stream_on(stream, here: int) -> int:
     return raw(here) if raw else torch.cuda.current_stream().cuda_stream
 
 
+def _bound(n: int) -> int:
+    """An upper bound as an int32 (ctypes would take the low bits): beyond the largest it bounds the same."""
+    return n if -1 <= n <= 0x7fffffff else 0x7fffffff if n > 0 else -1
+
+
 def _index(t, n: int, here: int, what: str):
     """Address of an int32 device array of n values (None: NULL)."""
     import torch
@@ -897,7 +902,7 @@ def op_cache_attention(cache: Cache, q, cu_q, rows, lens, max_q: int, max_len: i
         mask_at = _index(mask, n * words, here, "mask")
     a = WfCacheQuery(q.data_ptr(), out.data_ptr(), ldq, ldo, _index(cu_q, B + 1, here, "cu_q"), _index(rows, B, here, "rows"),
                      _index(lens, B, here, "lens"), mask_at, _index(mask_from, B, here, "mask_from"), None, 0, _torch_dtype_code(q.dtype),
-                     cols // 64, B, n, max_q, max_len, words, scale)
+                     cols // 64, B, n, _bound(max_q), _bound(max_len), words, scale)
     L, c, at = lib(), C.byref(cache._c), C.byref(a)
     workspace = _fill_workspace(a, L.wf_cache_attention_workspace(c, at), workspace, q, here, stream)
     _check(L.wf_op_cache_attention(c, at, _stream_on(stream, here)))
@@ -917,6 +922,8 @@ def op_beam_select(logits, scores, n_in=None, n_out=None, done=None, eos: int = 
     ld = stride[1] if W > 1 else stride[0] if B > 1 else V
     if B > 1 and W > 1 and stride[0] != W * ld:
         raise ValueError(f"logits: strides {stride}, need one row stride over streams and beams")
+    if V > 0x7fffffff or not -0x80000000 <= eos <= 0x7fffffff:
+        raise ValueError(f"n_vocab = {V}, eos = {eos}: need numbers of 32 bits")
     if scores.dtype != torch.float32 or (done is not None and done.dtype not in (torch.bool, torch.uint8)):
         raise TypeError("need float32 scores and, if any, done of bool or uint8")
     for t in (scores, done):
@@ -938,7 +945,7 @@ def op_beam_reorder(state, parents, lens=None, out=None, stream=None):
     [B, width]; lens int32 [B]: positions in use (None: all).  In place unless `out` is given."""
     here = _here(state, "state")
     shape, slots = state.shape, parents.numel()
-    if parents.dim() != 2 or len(shape) < 3 or shape[1] != slots:
+    if parents.dim() != 2 or len(shape) < 3 or shape[1] != slots or shape[0] > 0x7fffffff:
         raise ValueError(f"state: {tuple(shape)}, parents: {tuple(parents.shape)}: need [n_layers, B * width, n_pos, ..] and [B, width]")
     if out is None:
         out = state

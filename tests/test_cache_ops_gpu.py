@@ -592,3 +592,9 @@ def test_calls_do_not_follow_a_cache_whose_memory_moved():
                      lambda: wf.op_cache_attention(cache, q, *args, _i32([9]), 2, 9)):
             with pytest.raises(ValueError):
                 call()
+
+
+@pytest.mark.parametrize("act,cdtype", KINDS)
+def test_bounds_beyond_32_bits_bound_nothing(act, cdtype):
+    cache = _filled(90, 2, cdtype, 66)
+    _check_attention(cache, _q(7, 4, act, 67), [0, 3, 7], [0, 30], [71, 60], 2 ** 33 + 1, 2 ** 32 + 5)

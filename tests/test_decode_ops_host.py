@@ -214,6 +214,23 @@ def test_a_cache_keeps_to_the_memory_it_was_made_of(monkeypatch):
         c._here()
 
 
+@pytest.mark.parametrize("value", [1 << 31, (1 << 32) + 5, -(1 << 31) - 1], ids=str)
+def test_numbers_that_32_bits_do_not_hold(value, monkeypatch):
+    """The library's int32 would take such a number's low bits; an upper bound beyond every length is the largest one."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    logits = _fake((1, 1, max(value, 1)), torch.float32, P)
+    logits.stride = lambda: (logits.shape[2], logits.shape[2], 1)
+    scores, done = _fake((1, 1), torch.float32, P), _fake((1, 1), torch.uint8, P)
+    if value > 0:
+        with pytest.raises(ValueError, match="n_vocab"):
+            wf.op_beam_select(logits, scores)
+    logits = _fake((1, 1, 100), torch.float32, P)
+    logits.stride = lambda: (100, 100, 1)
+    with pytest.raises(ValueError, match="eos"):
+        wf.op_beam_select(logits, scores, done=done, eos=value)
+    assert wf._bound(value) == (0x7fffffff if value > 0 else -1) and wf._bound(77) == 77 and wf._bound(0x7fffffff) == 0x7fffffff
+
+
 # ---- the oracle's own pins ------------------------------------------------------------------------------------------------
 def test_oracle_format_is_torchs_e4m3():
     codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
