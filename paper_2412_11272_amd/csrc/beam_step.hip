@@ -148,7 +148,9 @@ __global__ void __launch_bounds__(256) beam_parts_kernel(SelectArgs p) {
     return;
   }
   // The sum: eight values in 32 bits, the rest in 64
-  const bool huge = fabsf(top) > 0x1p100f;      // top * kLog2e may overflow
+  // (the fused form's base is off from top * kLog2e by up to 2^-24 of it, which enters every exponential: harmless for ordinary logits, but 2^440 in a
+  // part at -1e10.  Differences from large maxima are exact wherever their exponential is not zero.)
+  const bool huge = fabsf(top) > 0x1p16f;
   const float base = top * kLog2e;
   double sum = 0.0;
   if (!huge) {

@@ -237,3 +237,37 @@ def test_selection_and_reordering_in_a_graph():
         want = start.clone()
         wf.op_beam_reorder(want, p, lens=lens)
         assert torch.equal(tok, t) and torch.equal(par, p) and torch.equal(score, s) and torch.equal(state, want), i
+
+
+@pytest.mark.parametrize("low", [-7e4, -1e9, -1e10, -3e15, -1e30, -3e38])
+@pytest.mark.parametrize("dtype", [F32, BF], ids=str)
+def test_logits_suppressed_by_a_large_finite_number(dtype, low):
+    # whole parts of a row, and whole rows, at a mask's value: the other tokens' totals do not feel it
+    x = _logits(1, 4, 9000, 21, dtype)
+    x[0, 0, 2048:] = low
+    x[0, 1, :8000] = low
+    x[0, 2, 5:] = low
+    x[0, 3, 4096:6144] = low * torch.linspace(1.0, 1.1, 2048).to(dtype).cuda()
+    tok, _ = _check_select(x, _scores(1, 4, 21))
+    assert (tok >= 0).all()
+
+
+@pytest.mark.parametrize("size", [6.5e4, 7e4, 1e7, 1e9, 1e10, 3.3e15, 1e25, 1.2e30, 1.3e30])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype", [F32, BF], ids=str)
+def test_rows_of_large_equal_logits(dtype, sign, size):
+    # each of V tokens at the same value x: log sum = x + log V, of which 64 bits keep |x| 2^-53, at the oracle's end and at the kernel's
+    B, W, V = 1, 3, 4500
+    x = torch.full((B, W, V), sign * size, device="cuda").to(dtype)
+    x[0, 1, 77:] = x[0, 1, 0] * (1 - sign * 2.0 ** -5)              # 77 tokens, all others far below
+    x[0, 2, 1:] = x[0, 2, 0] * (1 - sign * 2.0 ** -5)
+    sc = torch.full((B, W), -2.0, device="cuda")
+    tok, par, out, _ = wf.op_beam_select(x, sc)
+    xd = x.double().cpu().numpy()
+    rt, rp, rs, _ = D.beam_step(xd[0], np.full(W, -2.0), W, W)
+    assert np.isfinite(rs).all()
+    got = out[0].double().cpu().numpy()
+    # 2^-19 as stated, half a step of fp32, and 3 roundings of 64 bits of something of the logits' size on either side
+    assert (np.abs(got - rs) <= 2.0 ** -19 + 2.0 ** -24 * np.abs(rs) + 6 * 2.0 ** -53 * np.abs(xd).max()).all()
+    if size < 1e9:                                                  # there, log 77 and log 4500 are told apart
+        assert tok[0].tolist() == rt.tolist() and par[0].tolist() == rp.tolist() == [2, 1, 1]
