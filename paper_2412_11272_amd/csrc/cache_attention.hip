@@ -136,6 +136,13 @@ __device__ __forceinline__ f32x4 mma(const uint32_t (&a)[4], const uint32_t (&b)
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
 }
 
+// A product that is rounded, whatever is added to it: the largest logit is its reference then, of any size.  (fp32, where an instruction more
+// costs nothing next to the matrix instructions.)
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
 // A wave's running state for 16 query rows: lane (n, g) has row n's reference (in powers of two), its share of the sum, and values 16 g + 4 i + t.
 struct State {
   float m, l;
@@ -447,7 +454,7 @@ __global__ void __launch_bounds__(64 * NW, NQ == 1 && sizeof(T) == 2 ? 3 : 2) ca
         State &w = st[t0 + k];
         const float base = w.m == -INFINITY ? 0.0f : w.m;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[k][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k][j], c, -base));
+        for (int j = 0; j < 8; ++j) x[k][j] = __builtin_amdgcn_exp2f(BF ? __builtin_fmaf(x[k][j], c, -base) : rounded_product(x[k][j], c) - base);
         w.l += ((x[k][0] + x[k][1]) + (x[k][2] + x[k][3])) + ((x[k][4] + x[k][5]) + (x[k][6] + x[k][7]));
         if constexpr (NQ == 1) values(a, vt);      // once the keys' registers are free
         if constexpr (BF) {
@@ -505,16 +512,19 @@ __global__ void __launch_bounds__(64 * NW, NQ == 1 && sizeof(T) == 2 ? 3 : 2) ca
   const int64_t part_at = (((int64_t)s * H + h) * p.chunks + chunk) * 16 * NQ * p.n_split + z;      // of row 0 of the chunk; a row on: n_split
 
   // 0 x infinity and 0 x NaN of values that a row does not see, and infinity x the two parts of a weight, leave the result not finite, whatever
-  // follows.  Then, and only then, the rows are computed one by one.
+  // follows.  Next to a reference of 2^30 and more, rounded to whole numbers and coarser, products that are not rounded (bf16) give weights of 0 or
+  // infinity.  Then, and only then, the rows are computed one by one.
   if constexpr (BF || MASK) {
     bool fine = true;
 #pragma unroll
     for (int t = 0; t < NQ; ++t)
-      if (t * 16 + n16 < rows)
+      if (t * 16 + n16 < rows) {
+        if constexpr (BF) fine = fine && (fabsf(st[t].m) < 0x1p30f || st[t].m == -INFINITY);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) fine = fine && is_finite(st[t].o[i][e]);
+      }
     if (__syncthreads_or(!fine)) {
       const int to = (int)(split_from + p.split_keys < n ? split_from + p.split_keys : n);
       for (int local = wave; local < rows && local < 16 * NQ; local += NW) {

@@ -598,3 +598,32 @@ def test_calls_do_not_follow_a_cache_whose_memory_moved():
 def test_bounds_beyond_32_bits_bound_nothing(act, cdtype):
     cache = _filled(90, 2, cdtype, 66)
     _check_attention(cache, _q(7, 4, act, 67), [0, 3, 7], [0, 30], [71, 60], 2 ** 33 + 1, 2 ** 32 + 5)
+
+
+@pytest.mark.parametrize("n_keys", [40, 1700])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("act,cdtype", KINDS)
+def test_large_logits_still_share_out_the_weight(act, cdtype, masked, n_keys):
+    # q . k is one product of a few bits, the logit in powers of two is not: its rounded value is off by up to 2^-25 of it.  Equal logits share the
+    # weight, whatever their size; keys far below others have none.
+    for p in (20, 29, 31, 33, 34, 35, 40, 63, 100):
+        for sign in (1, -1):
+            cache = _filled(n_keys, 1, cdtype, 70)
+            k = torch.zeros((n_keys, 64))
+            k[:, 0] = sign * 1.625 * 2.0 ** p
+            if sign < 0:
+                k[n_keys - 3:, 0] = 0.0                # for the second sequence: three keys have all the weight
+            kd = k.to(act).cuda()
+            v = _np(wf.op_cache_read(cache, _i32([0, n_keys]), _i32([0]), n_keys, out_dtype=F32))[:, 64:]
+            wf.op_cache_write(cache, kd, torch.from_numpy(v).to(act).cuda(), _i32([0, n_keys]), _i32([0]))
+            v = _contents(cache)[:, 0, 1]
+            q = torch.zeros((20, 64), dtype=act, device="cuda")
+            q[:, 0] = 1.3984375
+            mask = torch.full((20, -(-n_keys // 32)), -1, dtype=torch.int32, device="cuda") if masked else None
+            for scale in (0.1, 0.125, 0.3):
+                lens = [n_keys - 3, n_keys]
+                out = _np(wf.op_cache_attention(cache, q, _i32([0, 1, 20]), _i32([0, 0]), _i32(lens), 19, n_keys, scale=scale, mask=mask))
+                for rows, w in ((out[:1], v[:lens[0]]), (out[1:], v[n_keys - 3:] if sign < 0 and p > 20 else v if sign > 0 else None)):
+                    if w is not None:
+                        tol = _tolerance(act, len(w), w.mean(0), np.abs(w).mean(0), 0.0)
+                        assert (np.abs(rows - w.mean(0)) <= tol).all(), (p, sign, scale, len(w))
