@@ -527,7 +527,8 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  *                     shared out, and with it the last bits of a result, goes by the bounds and counts of the call, not by the lengths.
  * wf_op_beam_select   one step of a beam search, per stream s of B with n_in[s] beams (DEVICE int32 [B]; NULL: width; clamped to 0 .. width):
  *                     candidates (b, t) of all beams b and tokens t with total(b, t) = score_in[s, b] + logits[s, b, t] - log sum exp
- *                     logits[s, b, :], in 64 bits.  The n_out[s] (NULL: width) best come out, best first: tokens of one beam by
+ *                     logits[s, b, :], in 64 bits but for the exponentials and their sums of eight, which are fp32: the log sum of a row is off by less
+ *                     than 2^-19 (2^-22 as a rule), the same for equal rows, and totals of two beams that are nearer than 2^-18 may come in either order.  The n_out[s] (NULL: width) best come out, best first: tokens of one beam by
  *                     their logits and then the lowest token, beams among each other by the totals and then the lowest beam.  logits_dev
  *                     [B, width, n_vocab] f32 or bf16 with row stride ld elements (a multiple of nothing); logits and scores that are not finite
  *                     take no part.  done_in (uint8 [B, width], NULL: none): a beam that is done has one candidate, token eos at its

@@ -271,3 +271,34 @@ def test_rows_of_large_equal_logits(dtype, sign, size):
     assert (np.abs(got - rs) <= 2.0 ** -19 + 2.0 ** -24 * np.abs(rs) + 6 * 2.0 ** -53 * np.abs(xd).max()).all()
     if size < 1e9:                                                  # there, log 77 and log 4500 are told apart
         assert tok[0].tolist() == rt.tolist() and par[0].tolist() == rp.tolist() == [2, 1, 1]
+
+
+@pytest.mark.parametrize("V", [300, 5001, 51866])
+@pytest.mark.parametrize("dtype", [F32, BF], ids=str)
+def test_beams_whose_rows_are_permutations_of_each_other(dtype, V):
+    # their log sums are equal, the kernel's within 2^-18 of each other: nearer totals come in any order, others in their own
+    W = 6
+    g = torch.Generator().manual_seed(V)
+    row = torch.randn(V, generator=g) * 2.5
+    row[7] = row.max() + 2.0                                    # each beam's first candidate is ahead of every second one
+    x = torch.stack([row[torch.randperm(V, generator=g)] for _ in range(W)])[None].to(dtype).cuda()
+    best = x[0].float().argmax(1).tolist()
+    xd = x[0].double().cpu().numpy()
+    lse = np.log(np.exp(xd[0] - xd[0].max()).sum()) + xd[0].max()
+    gap = np.sort(xd[0])[-1] - np.sort(xd[0])[-2]
+    assert gap > 1.0
+
+    def select(scores):
+        tok, par, out, _ = wf.op_beam_select(x, torch.tensor([scores], dtype=torch.float32, device="cuda"))
+        return tok[0].tolist(), par[0].tolist(), out[0].double().cpu().numpy()
+
+    tok, par, out = select([-1.0] * W)
+    assert sorted(par) == list(range(W)) and tok == [best[p] for p in par]
+    total = -1.0 + xd[0].max() - lse
+    assert (np.abs(out - total) <= 2.0 ** -19 + 2.0 ** -24 * abs(total)).all()
+    order = [4, 0, 5, 2, 1, 3]
+    scores = [0.0] * W
+    for i, b in enumerate(order):
+        scores[b] = -1.0 - i * 2.0 ** -17
+    tok, par, _ = select(scores)
+    assert par == order and tok == [best[b] for b in order]
