@@ -645,9 +645,16 @@ struct Plan {
   int nq, nw, chunks, n_split, split_keys;
 };
 
-// Query rows of a workgroup: 16, 32 or 64 (fp32: 32, more outgrow the registers).  Rows beyond that read the keys again, from the L2: trees of 68 .. 160
-// rows over 20 000 .. 65 536 bf16 keys take 140 us with 64, 160 with 32; 64 rows over 1500 keys of 20 heads 41 and 43 (in 8 bits, where a
-// tile's conversion weighs more but the tiles are half as many bytes, 34 and 29).
+// Query rows of a workgroup: 16, 32 or 64.  Rows beyond that read the keys again, from the L2.  What decides is what the reading weighs:
+//   bf16 over bf16: trees of 68 .. 160 rows over 20 000 .. 65 536 keys of 8 heads take 168 us with 64, 205 with 32; 16 x 64 rows over 1500 keys of 20
+//     heads 41 and 44;
+//   bf16 over 8 bits, half the bytes: 32 where two workgroups hold all rows (16 x 64 rows over 1500 keys of 20 heads 32 us with 32, 37 with 64;
+//     64 x 64 over 51 .. 1525 62 and 69; 4 x 64 over 48 000 keys of 8 heads 78 and 92; but 64 x 64 over 1500 of 8 heads 43 and 39), and 64 beyond (132
+//     rows over 4 x 40 000 keys of 8 heads 183 us with 32, 158 with 64; over 16 x 1500 26 and 32);
+//   fp32 over fp32: 32 (16 x 64 rows over 1500 keys of 20 heads 90 us, 106 with 16; under a mask 97 and 109, though that kernel spills five registers;
+//     64 do not fit);
+//   fp32 over 8 bits: 16, its fp32 products outweigh a quarter of the bytes (16 x 64 rows over 1500 keys of 20 heads 79 us, 90 with 32; 32 over
+//     4 x 20 000 of 8 heads 61 and 74; trees as above 627 and 623).
 // Workgroups: keys are split where a chip of 256 compute units would not get four (eight, if they have more than 16 rows and so last long and unevenly)
 // each: one token over 65 536 keys of 8 heads in 8 bits 23.2 us with 1024, 23.8 with 2048; the trees 163 and 147.  A part keeps 768 keys: below, joining costs more
 // than it wins (1500 keys of 20 heads: 12.6 us in one part, 17 in two; 8 x 8192 keys of 8 heads in bf16 39 us with 1024 a part, 35.5 with 512).
@@ -656,7 +663,8 @@ struct Plan {
 Plan plan_of(const wf_cache &c, const wf_cache_query &a) {
   Plan p{};
   const int64_t rows = (int64_t)std::min(a.max_q, std::max(a.n_q_rows, 1)) * (a.n_heads / c.n_heads);
-  p.nq = rows <= 16 ? 1 : rows <= 32 || a.dtype == WF_DTYPE_F32 ? 2 : 4;
+  const bool f8 = c.dtype == WF_DTYPE_F8;
+  p.nq = rows <= 16 || (f8 && a.dtype == WF_DTYPE_F32) ? 1 : rows <= (f8 ? 64 : 32) || a.dtype == WF_DTYPE_F32 ? 2 : 4;
   p.chunks = (int)((rows + 16 * p.nq - 1) / (16 * p.nq));
   const int64_t groups = (int64_t)a.n_seqs * c.n_heads * p.chunks, want = p.nq > 1 ? 2048 : 1024;
   int64_t n = groups >= want ? 1 : (want + groups - 1) / groups;
@@ -678,8 +686,10 @@ void launch_attend(const AttendArgs &p, const Plan &plan, dim3 grid, hipStream_t
   if (plan.nq == 1 && plan.nw == 1) launch_attend<T, CACHE, 1, 1>(p, grid, s);
   else if (plan.nq == 1 && plan.nw == 2) launch_attend<T, CACHE, 1, 2>(p, grid, s);
   else if (plan.nq == 1) launch_attend<T, CACHE, 1, 4>(p, grid, s);
-  else if (plan.nq == 2) launch_attend<T, CACHE, 2, 4>(p, grid, s);
-  else if constexpr (sizeof(T) == 2) launch_attend<T, CACHE, 4, 4>(p, grid, s);
+  else if constexpr (sizeof(T) == 2 || CACHE == WF_DTYPE_F32) {
+    if (plan.nq == 2) launch_attend<T, CACHE, 2, 4>(p, grid, s);
+    else if constexpr (sizeof(T) == 2) launch_attend<T, CACHE, 4, 4>(p, grid, s);
+  }
 }
 
 }  // namespace

@@ -627,3 +627,20 @@ def test_large_logits_still_share_out_the_weight(act, cdtype, masked, n_keys):
                     if w is not None:
                         tol = _tolerance(act, len(w), w.mean(0), np.abs(w).mean(0), 0.0)
                         assert (np.abs(rows - w.mean(0)) <= tol).all(), (p, sign, scale, len(w))
+
+
+@pytest.mark.parametrize("length", [60, 200])
+@pytest.mark.parametrize("n_q", [9, 20])
+@pytest.mark.parametrize("act,cdtype", KINDS)
+def test_many_short_sequences_of_several_row_chunks(act, cdtype, n_q, length):
+    # 18 and 40 rows a key head; where a workgroup has 16 of them it may have one or two waves as well
+    B, H = 70, 8
+    lens = [(length * (i % 6)) // 5 for i in range(B)]
+    rows = [(i * 53) % 700 for i in range(B)]
+    cache = _filled(900, H, cdtype, 68)
+    q = _q(B * n_q, 2 * H, act, 69)
+    cu = [i * n_q for i in range(B + 1)]
+    some = {0, n_q - 1, n_q, 5 * n_q + 8, B * n_q - 1}
+    _check_attention(cache, q, cu, rows, lens, n_q, length, heads=[0, 15], some_rows=some)
+    words = torch.from_numpy(np.random.default_rng(70).integers(0, 1 << 32, (B * n_q, 2), dtype=np.uint32).view(np.int32)).cuda()
+    _check_attention(cache, q, cu, rows, lens, n_q, length, heads=[0, 15], some_rows=some, mask=words, since=[max(0, n - 40) for n in lens])
