@@ -490,7 +490,7 @@ void wf_beam_pruner_destroy(wf_beam_pruner *p);  /* NULL-safe */
  * What runs on the GPU for every new token after wf_prefill.  Operators on caller-provided DEVICE buffers like wf_op_linear and its kind,
  * all asynchronous on hip_stream, none allocates, waits or copies, so they can be captured into a graph.  What changes from
  * step to step (lengths, rows, parents) is read from device memory, so that one captured graph serves every step; the host arguments are
- * upper bounds.  Device values that lie outside their bounds never lead to an access outside the buffers: such rows or slots are
+ * upper bounds.  Counts of streams and sequences are at least 1; no tokens, rows, layers or positions are nothing to do.  Device values that lie outside their bounds never lead to an access outside the buffers: such rows or slots are
  * left out, as stated with each operator.  All work of a call is ordered on its stream; two calls may overlap if their outputs and
  * workspaces are their own.  Sources, caches and outputs of one call must not overlap unless it is said below.
  *

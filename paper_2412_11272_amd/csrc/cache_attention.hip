@@ -4,10 +4,12 @@
 // Bound by memory: a key / value pair of a head is 256 bytes in bf16 (130 in 8 bits) and serves only the query rows that share the
 // head (queries of the sequence times query heads per key head), so the cache goes from memory straight to registers, once,
 // and nothing of it through the LDS.  A workgroup has one key / value head of one sequence, up to 16 * NQ of its query rows and a range of keys; its
-// waves take tiles of 32 keys in turn, each with a running maximum and sum of its own, and join in the LDS at the end.  Measured on one MI355X (a
-// read-only pass over memory in this pattern reaches 5.3 .. 5.8 TB/s): 320 sequences of 512 keys of 20 heads 6.06 TB/s in bf16, 5.63 in 8 bits, 6.14 in fp32;
-// five beams each of 64 streams of 51 .. 1525 keys 4.5, 3.8 and 4.9, held up by the uneven lengths; trees of 68 .. 160 rows are held up by the
-// softmax's and the weights' instructions, 2.1 TB/s and 260 TFLOP/s.
+// waves take tiles of 32 keys in turn, each with a running maximum and sum of its own, and join in the LDS at the end.  Measured on one MI355X (reading
+// alone reaches 6.2 TB/s): 320 sequences of 512 keys of 20 heads 6.1 TB/s in bf16, 5.5 in 8 bits, 6.2 in fp32; five beams each of 64 streams of
+// 51 .. 1525 keys 4.4, 3.6 and 4.5 (57, 36 and 111 us): 1280 workgroups on 768 or, in 8 bits, 1024 places leave a last round partly filled (720 keys each:
+// 4.9, 4.0 and 4.7), and the uneven lengths cost the rest; trees of 68 .. 160 rows are held up by the softmax's and the weights' instructions, 2.1 TB/s and
+// 260 TFLOP/s.  fp32 queries over 8 bits are bound by the fp32 matrix instructions, 64 of 32 cycles a tile whatever it weighs: 3.0 TB/s, and 67 us for
+// the beams; such trees 520 us over fp32, 640 over 8 bits.
 //
 // A tile's products, on the 16 x 16 matrix instructions, run transposed like those of the prefill attention: S^T = K Q^T, O^T = V^T P^T.
 // A lane (n = lane % 16, g = lane / 16) then holds
@@ -19,8 +21,10 @@
 //   O^T               query n, values 16 g + 4 i + t from the t-th of four instructions (which takes value 4 n + t of each lane's keys)
 // What remains between loading V and multiplying is to pair two keys' values in a register: one byte permutation for two of them.
 //
-// Rounding: logits, statistics and sums are fp32.  Next to bf16 the weights enter as the sum of two bf16 parts (2^-17 of a weight is lost, where
-// one part would lose 2^-9): twice the second product's instructions, of which the kernel has plenty to spare.  Values of the 8-bit caches with their
+// Rounding: logits, statistics and sums are fp32.  Next to bf16 the weights enter as the sum of two bf16 parts (2^-18 of a weight is lost, where
+// one part would lose 2^-9, and the output's rounding 2^-9 of the result): twice the second product's instructions.  A third part would keep all 24 bits; it
+// leaves the error against 64 bits as it is (trees, relative: 1.66440e-3 either way) and takes 156 us for the trees instead of 138, 35.5 for beams instead
+// of 33.5.  Values of the 8-bit caches with their
 // powers of two are exact as fp32 operands, and as bf16 operands from 2^-124 on.
 #include "cache_device.h"
 #include "host_runtime.h"
@@ -382,7 +386,7 @@ __global__ void __launch_bounds__(64 * NW, NQ == 1 && sizeof(T) == 2 ? 3 : 2) ca
         for (int i = 0; i < QD; ++i) kt[u][i] = a.k[u][i];
       }
     }
-    // Two query tiles side by side: one's matrix instructions beside the other's exponentials
+    // Two query tiles side by side: one's matrix instructions beside the other's exponentials.  (Behind an odd number of tiles an empty one is computed.)
     constexpr int GT = NQ < 2 ? NQ : 2;
 #pragma unroll
     for (int t0 = 0; t0 < NQ; t0 += GT) {
@@ -513,7 +517,9 @@ __global__ void __launch_bounds__(64 * NW, NQ == 1 && sizeof(T) == 2 ? 3 : 2) ca
 
   // 0 x infinity and 0 x NaN of values that a row does not see, and infinity x the two parts of a weight, leave the result not finite, whatever
   // follows.  Next to a reference of 2^30 and more, rounded to whole numbers and coarser, products that are not rounded (bf16) give weights of 0 or
-  // infinity.  Then, and only then, the rows are computed one by one.
+  // infinity.  Then, and only then, the rows are computed one by one: all of the workgroup, since what one row does not see spoils every other that shares
+  // the tile, and slowly, a lane a key (one key of NaN in each head: 64 x 5 beams of 20 heads where it is in one stream's cache 57 -> 261 us,
+  // in 8 bits 36 -> 467; hidden in one of four trees 166 us -> 9 ms).
   if constexpr (BF || MASK) {
     bool fine = true;
 #pragma unroll
@@ -656,8 +662,9 @@ struct Plan {
 //   fp32 over 8 bits: 16, its fp32 products outweigh a quarter of the bytes (16 x 64 rows over 1500 keys of 20 heads 79 us, 90 with 32; 32 over
 //     4 x 20 000 of 8 heads 61 and 74; trees as above 627 and 623).
 // Workgroups: keys are split where a chip of 256 compute units would not get four (eight, if they have more than 16 rows and so last long and unevenly)
-// each: one token over 65 536 keys of 8 heads in 8 bits 23.2 us with 1024, 23.8 with 2048; the trees 163 and 147.  A part keeps 768 keys: below, joining costs more
-// than it wins (1500 keys of 20 heads: 12.6 us in one part, 17 in two; 8 x 8192 keys of 8 heads in bf16 39 us with 1024 a part, 35.5 with 512).
+// each: one token over 65 536 keys of 8 heads in 8 bits 23.2 us with 1024, 23.8 with 2048; the trees 163 and 147.  A part keeps 768 keys, between what short and
+// what long sequences want: with 512, 1100 keys (then in two parts) of 20 heads take 12.4 us instead of 10.9, 30 sequences of them in 8 bits 27 instead of 24,
+// 8192 keys of 20 heads 16.1 and 15.2; but 8 x 8192 keys of 8 heads 34.8 instead of 39.4, 16 x 4096 36.3 and 39.1.
 // Waves: four share a sequence's tiles; where sequences are short and many, two or one (320 of them, 20 heads, 8 bits: 32 keys 26.5 us with four, 16.9 with
 // two, 12.6 with one; 128 keys 37.1, 27.5, 25.5; 256 keys 47.7, 42.3, 43.2; 512 keys 75.9, 77.1, 80.4).
 Plan plan_of(const wf_cache &c, const wf_cache_query &a) {
